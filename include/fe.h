@@ -60,8 +60,9 @@ enum {
   FE_ERR_TIMEOUT = 8        /* a bounded device-side wait gave up; results are invalid   */
 };
 
-/* Element type of the context / pool inputs. */
-enum { FE_IO_BF16 = 0, FE_IO_F32 = 1 };
+/* Element type of the context / pool inputs; FE_IO_F16 is taken by the
+ * candidate generator's operators alone (fe_kv_append and what follows it). */
+enum { FE_IO_BF16 = 0, FE_IO_F32 = 1, FE_IO_F16 = 2 };
 
 typedef struct fe_config {
   int32_t d;          /* model width; multiple of 32, 32 <= d <= 512                  */
@@ -358,6 +359,159 @@ int fe_debug_alloc_hook(int fail_at, int64_t* live_out);
  * host submissions outstanding), FE_ERR_CUDA.
  */
 int fe_debug_wait_probe(fe_ctx* ctx, uint32_t limit_us, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Operators of the candidate generator (no counterpart in the paper, which
+ * takes the K candidate sequences of a request as given): a language model that
+ * writes a request's candidates token by token from the request's context, and
+ * learns from the scores that fe_evaluate gives them.  They need no fe_ctx,
+ * allocate nothing, keep nothing between calls, and enqueue on `stream`
+ * (a cudaStream_t) without waiting; calls on different streams are
+ * independent as long as their outputs, pages written and workspaces differ.
+ * They can be captured in a CUDA graph.  Every pointer is a device pointer;
+ * arguments the host can see are checked before anything is enqueued, indices
+ * in device memory by the kernels, which OR FE_ST_INDEX into *status (a device
+ * word that the caller clears; NULL: not reported) and confine the damage to the
+ * sequence or row concerned, as each entry point says.
+ * ---------------------------------------------------------------------------
+ */
+
+/* Bits of a device status word. */
+enum { FE_ST_INDEX = 1, FE_ST_NUMERIC = 2, FE_ST_TIMEOUT = 4 };
+
+/* The pairs that a rotation by position turns: (x_i, x_{i + rot/2}) or (x_2i, x_{2i+1}). */
+enum { FE_PAIRS_HALF = 0, FE_PAIRS_INTERLEAVED = 1 };
+
+/*
+ * Paged keys and values: pages of page_rows rows, [n_pages, kv_heads, page_rows,
+ * head_dim] each, in bf16 or f16.  Row c of a sequence is place c % page_rows of the
+ * page that entry c / page_rows of its page-table row names.  Prefixes and
+ * sequences share the pages.
+ */
+typedef struct fe_paged_kv {
+  int32_t dtype;      /* FE_IO_BF16 or FE_IO_F16                                   */
+  int32_t n_pages;    /* n_pages * kv_heads * page_rows < 2^31                     */
+  int32_t page_rows;  /* 16, 32, 64 or 128                                         */
+  int32_t kv_heads;   /* >= 1                                                      */
+  int32_t head_dim;   /* 32, 64 or 128                                             */
+  void* k;            /* 128-byte aligned                                          */
+  void* v;
+} fe_paged_kv;
+
+/*
+ * Append rows to paged sequences.  Sequence s (of n_seqs) gets the input rows
+ * row_start[s] .. row_start[s + 1] - 1 (possibly none); the j-th of them becomes its
+ * row first[s] + j, at position shift[s] + first[s] + j.  Keys, and the queries of the
+ * same rows when q is given, are rotated by their position p on the way: with
+ * (c, s) = rope[p][i], pair i becomes (x c - y s, y c + x s); elements from rot_dim
+ * on are copied, as values are.  Products and sums are fp32, rounded once.
+ *   row_start [n_seqs + 1] int32, not decreasing, first 0, last n_rows
+ *   first     [n_seqs] int32    rows that the sequence holds already
+ *   shift     [n_seqs] int32    position of its row 0 (after a shared prefix, the
+ *                               prefix's length); NULL: 0
+ *   pages     [n_seqs, page_cols] int32
+ *   k, v      [n_rows, kv_heads, head_dim], q [n_rows, q_heads, head_dim]: the
+ *             pages' type, rows and heads apart by the given strides (elements,
+ *             multiples of 8), 16-byte aligned; q_out contiguous, may be q when that is
+ *   rope      [rope_rows, rot_dim / 2, 2] fp32, 16-byte aligned: cosine and sine;
+ *             NULL: no rotation.  rot_dim: a multiple of 16, at most head_dim
+ * Two rows must not name the same place.  A row whose page entry is outside
+ * [0, n_pages) or past page_cols is not stored; a row whose position is outside
+ * rope gets NaN for its rotated elements: FE_ST_INDEX.
+ * Errors: FE_ERR_INVALID_ARG, FE_ERR_UNSUPPORTED, FE_ERR_CUDA.
+ */
+typedef struct fe_append_args {
+  fe_paged_kv kv;
+  int32_t n_seqs, n_rows, page_cols, q_heads, rope_rows, rot_dim, pairs, reserved;
+  const int32_t *row_start, *first, *shift, *pages;
+  const void *k, *v, *q;
+  int64_t k_row, k_head, v_row, v_head, q_row, q_head; /* strides in elements */
+  void* q_out;
+  const float* rope;
+  int32_t* status;
+} fe_append_args;
+int fe_kv_append(const fe_append_args* args, void* stream);
+
+/*
+ * Attention of sequences that share a prefix.  The sequences group_start[g] ..
+ * group_start[g + 1] - 1 form group g, and all of them see the prefix_len[g] rows of its
+ * prefix; the n_s = row_start[s + 1] - row_start[s] query rows of sequence s are the
+ * last n_s of its own seq_len[s] rows (which the pages already hold), so the j-th sees
+ * its own rows 0 .. seq_len[s] - n_s + j.  Query head h reads key head
+ * h / (q_heads / kv_heads).
+ *   out[t, h] = sum_k p_k v_k,  p = softmax(scale q . k) over the rows seen
+ *   lse[t, h] = log sum_k exp(scale q . k)
+ * A row that sees nothing gets out = 0 and lse = -inf.  Rows of the pages past a
+ * sequence's length are never part of a result, whatever they hold (NaN too).
+ *   q [n_rows, q_heads, head_dim] in the pages' type, strides as in fe_append_args;
+ *   out [n_rows, q_heads, head_dim] contiguous, in the same type, 16-byte aligned;
+ *   lse [n_rows, q_heads] fp32 or NULL
+ *   group_start [n_groups + 1] int32, not decreasing, first 0, last n_seqs
+ *   prefix_pages [n_groups, prefix_cols], pages [n_seqs, page_cols] int32
+ * Softmax statistics and accumulators are fp32.  The result does not depend on the
+ * timing of the run.  A page entry outside [0, n_pages), or a length that is negative
+ * or does not fit the page table, makes the rows that see it NaN: FE_ST_INDEX.
+ * The workspace (fe_prefix_attention_workspace bytes for the same args, 256-byte
+ * aligned) is the call's own until it has run; what it holds before is of no
+ * importance.  fe_prefix_attention_workspace returns 0 for arguments that are refused.
+ * Errors: FE_ERR_INVALID_ARG, FE_ERR_UNSUPPORTED, FE_ERR_WORKSPACE (too
+ * small), FE_ERR_CUDA.
+ */
+typedef struct fe_prefix_args {
+  fe_paged_kv kv;
+  int32_t n_groups, n_seqs, n_rows, q_heads, prefix_cols, page_cols;
+  float scale;
+  int32_t reserved;
+  const int32_t *group_start, *prefix_len, *prefix_pages;
+  const int32_t *row_start, *seq_len, *pages;
+  const void* q;
+  int64_t q_row, q_head; /* strides in elements */
+  void* out;
+  float* lse;
+  void* workspace;
+  uint64_t workspace_bytes;
+  int32_t* status;
+} fe_prefix_args;
+uint64_t fe_prefix_attention_workspace(const fe_prefix_args* args);
+int fe_prefix_attention(const fe_prefix_args* args, void* stream);
+
+/*
+ * Clipped policy loss with a KL term.  For token t = 0 .. rows - 1, with
+ * x = logits[t] / temperature, y = tokens[t], A = advantages[t], w = weights[t]:
+ *   lse = log sum_v exp(x_v)        logp = x_y - lse
+ *   r = exp(logp - old_logp[t])     d = ref_logp[t] - logp
+ *   terms[t] = w [ -min(r A, clamp(r, 1 - clip_low, 1 + clip_high) A) + beta (exp(d) - d - 1) ]
+ *   coef[t] = d terms[t] / d logp   (the clipped branch has slope 0; where both branches
+ *                                    are equal the slope is -A r)
+ *   loss = sum_t terms[t]           (in a fixed order)
+ *   grad[t, v] = grad_scale coef[t] (1[v = y] - exp(x_v - lse)) / temperature
+ *   logits [rows, vocab] bf16, f16 or fp32, rows logits_row elements apart, any
+ *          alignment of the type; grad the same type, rows grad_row apart (fastest when
+ *          both have the same alignment), may be logits itself; NULL: not computed
+ *   tokens [rows] int32, advantages [rows]; weights [rows] or NULL (1 / rows each);
+ *   old_logp [rows] or NULL (the present policy: r = 1); ref_logp [rows] or NULL (no KL
+ *          term); loss [1], terms, logp, lse, coef [rows]: fp32
+ * A token of weight 0 takes no part: its logits are not read, its outputs and its
+ * gradient are 0.  A token outside [0, vocab) gets NaN throughout: FE_ST_INDEX.
+ * Logits of -inf have probability 0.
+ * fe_policy_loss_backward writes grad alone, from the lse and coef of an earlier call
+ * (weights and the tokens' order unchanged) times *upstream (a device float, NULL: 1).
+ * Errors: FE_ERR_INVALID_ARG, FE_ERR_UNSUPPORTED, FE_ERR_CUDA.
+ */
+typedef struct fe_policy_args {
+  int32_t dtype, rows, vocab;
+  float clip_low, clip_high, beta, temperature, grad_scale;
+  const void* logits;
+  int64_t logits_row, grad_row; /* strides in elements */
+  const int32_t* tokens;
+  const float *advantages, *weights, *old_logp, *ref_logp;
+  float *loss, *terms, *logp, *lse, *coef;
+  void* grad;
+  int32_t* status;
+} fe_policy_args;
+int fe_policy_loss(const fe_policy_args* args, void* stream);
+int fe_policy_loss_backward(const fe_policy_args* args, const float* upstream, void* stream);
 
 /* Release every device resource owned by ctx (waits for its work first). */
 int fe_destroy(fe_ctx* ctx);

@@ -26,6 +26,10 @@ FE_ERR_NUMERIC = 7
 FE_ERR_TIMEOUT = 8
 FE_IO_BF16 = 0
 FE_IO_F32 = 1
+FE_IO_F16 = 2
+FE_ST_INDEX = 1
+FE_ST_NUMERIC = 2
+FE_ST_TIMEOUT = 4
 
 EXPORTS = ["fe_weight_count", "fe_init", "fe_reserve", "fe_evaluate", "fe_evaluate_async", "fe_last_status",
            "fe_evaluate_host", "fe_evaluate_factorized", "fe_submit_host", "fe_wait_host", "fe_debug_layout",
@@ -33,7 +37,9 @@ EXPORTS = ["fe_weight_count", "fe_init", "fe_reserve", "fe_evaluate", "fe_evalua
            "fe_profile_read",
            "fe_kernels_per_batch", "fe_distinct_layout_noalloc", "fe_destroy", "fe_strerror",
            "fe_last_error_message", "fe_blob_parse", "fe_init_blob", "fe_debug_alloc_hook",
-           "fe_debug_wait_probe", "fe_debug_keep_intermediates"]
+           "fe_debug_wait_probe", "fe_debug_keep_intermediates",
+           "fe_kv_append", "fe_prefix_attention_workspace", "fe_prefix_attention", "fe_policy_loss",
+           "fe_policy_loss_backward"]
 
 
 class FeConfig(ctypes.Structure):
@@ -42,6 +48,40 @@ class FeConfig(ctypes.Structure):
                 ("ln_eps", ctypes.c_float), ("n_tasks", ctypes.c_int32), ("no_cross_seq", ctypes.c_int32),
                 ("elem_self_attn", ctypes.c_int32), ("encode_pool", ctypes.c_int32),
                 ("linear_context_attn", ctypes.c_int32)]
+
+
+class FePagedKv(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p)]
+
+
+class FeAppendArgs(ctypes.Structure):
+    _fields_ = ([("kv", FePagedKv)]
+                + [(n, ctypes.c_int32) for n in ("n_seqs", "n_rows", "page_cols", "q_heads", "rope_rows", "rot_dim",
+                                                 "pairs", "reserved")]
+                + [(n, ctypes.c_void_p) for n in ("row_start", "first", "shift", "pages", "k", "v", "q")]
+                + [(n, ctypes.c_int64) for n in ("k_row", "k_head", "v_row", "v_head", "q_row", "q_head")]
+                + [(n, ctypes.c_void_p) for n in ("q_out", "rope", "status")])
+
+
+class FePrefixArgs(ctypes.Structure):
+    _fields_ = ([("kv", FePagedKv)]
+                + [(n, ctypes.c_int32) for n in ("n_groups", "n_seqs", "n_rows", "q_heads", "prefix_cols", "page_cols")]
+                + [("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+                + [(n, ctypes.c_void_p) for n in ("group_start", "prefix_len", "prefix_pages", "row_start", "seq_len",
+                                                  "pages", "q")]
+                + [(n, ctypes.c_int64) for n in ("q_row", "q_head")]
+                + [(n, ctypes.c_void_p) for n in ("out", "lse", "workspace")]
+                + [("workspace_bytes", ctypes.c_uint64), ("status", ctypes.c_void_p)])
+
+
+class FePolicyArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "rows", "vocab")]
+                + [(n, ctypes.c_float) for n in ("clip_low", "clip_high", "beta", "temperature", "grad_scale")]
+                + [("logits", ctypes.c_void_p), ("logits_row", ctypes.c_int64), ("grad_row", ctypes.c_int64)]
+                + [(n, ctypes.c_void_p) for n in ("tokens", "advantages", "weights", "old_logp", "ref_logp", "loss",
+                                                  "terms", "logp", "lse", "coef", "grad", "status")])
 
 
 class FeError(RuntimeError):
@@ -100,6 +140,16 @@ def load_library(path: str = LIB_PATH):
     L.fe_kernels_per_batch.restype = i32
     L.fe_distinct_layout_noalloc.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp]
     L.fe_distinct_layout_noalloc.restype = i32
+    L.fe_kv_append.argtypes = [ctypes.POINTER(FeAppendArgs), vp]
+    L.fe_kv_append.restype = i32
+    L.fe_prefix_attention_workspace.argtypes = [ctypes.POINTER(FePrefixArgs)]
+    L.fe_prefix_attention_workspace.restype = ctypes.c_uint64
+    L.fe_prefix_attention.argtypes = [ctypes.POINTER(FePrefixArgs), vp]
+    L.fe_prefix_attention.restype = i32
+    L.fe_policy_loss.argtypes = [ctypes.POINTER(FePolicyArgs), vp]
+    L.fe_policy_loss.restype = i32
+    L.fe_policy_loss_backward.argtypes = [ctypes.POINTER(FePolicyArgs), vp, vp]
+    L.fe_policy_loss_backward.restype = i32
     L.fe_destroy.argtypes = [vp]
     L.fe_destroy.restype = i32
     L.fe_strerror.argtypes = [i32]

@@ -24,6 +24,31 @@ int set_cuda_err(cudaError_t e, const char* what) {
   return FE_ERR_CUDA;
 }
 
+}  // namespace
+
+// the operators' way to the same message (no exception leaves: a message that cannot be
+// stored is dropped)
+namespace fe {
+int fail(int code, const char* msg) noexcept {
+  try {
+    g_msg = msg;
+  } catch (...) {
+    g_msg.clear();
+  }
+  return code;
+}
+int fail_cuda(cudaError_t e, const char* what) noexcept {
+  try {
+    return set_cuda_err(e, what);
+  } catch (...) {
+    g_msg.clear();
+    return FE_ERR_CUDA;
+  }
+}
+}  // namespace fe
+
+namespace {
+
 // Every device and page-locked allocation of the library goes through
 // dev_alloc / host_alloc: they count the live allocations and, for tests
 // (fe_debug_alloc_hook), can make a chosen allocation fail as if the device
