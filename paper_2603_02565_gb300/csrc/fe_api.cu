@@ -12,6 +12,7 @@
 
 #include "fe.h"
 #include "fe_kernels.h"
+#include "fe_ops.cuh"
 
 using fe::bf16;
 
@@ -108,9 +109,7 @@ inline int round_up(int x, int m) { return (x + m - 1) / m * m; }
 // ---------------------------------------------------------------------------
 // TMA descriptor encoding (driver entry point, no link-time libcuda dependency)
 // ---------------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+using fe::EncodeTiledFn;
 
 EncodeTiledFn encode_fn() {
   static EncodeTiledFn fn = nullptr;
@@ -124,6 +123,12 @@ EncodeTiledFn encode_fn() {
   }
   return fn;
 }
+
+}  // namespace
+namespace fe {
+EncodeTiledFn encode_tiled_fn() noexcept { return encode_fn(); }
+}  // namespace fe
+namespace {
 
 // A bf16 matrix stored as one or two planes (hi, lo), row-major [rows, ld].
 // A bf16 hi/lo pair of row-major planes, or (attention operands: context K/V,

@@ -10,6 +10,12 @@ namespace fe {
 int fail(int code, const char* msg) noexcept;
 int fail_cuda(cudaError_t e, const char* what) noexcept;
 
+// cuTensorMapEncodeTiled by its driver entry point (fe_api.cu); null when unavailable.
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn() noexcept;
+
 template <typename T>
 struct Elem;
 template <>
@@ -25,6 +31,11 @@ struct Elem<__nv_bfloat16> {
     a = bf16lo_f(w);
     b = bf16hi_f(w);
   }
+  __device__ static __forceinline__ uint32_t zero_fma(uint32_t w, uint32_t acc) {  // 0 w + acc, both halves
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(w), "r"(0u), "r"(acc));
+    return r;
+  }
 };
 template <>
 struct Elem<__half> {
@@ -36,6 +47,11 @@ struct Elem<__half> {
     const float2 f = __half22float2(*reinterpret_cast<__half2*>(&w));
     a = f.x;
     b = f.y;
+  }
+  __device__ static __forceinline__ uint32_t zero_fma(uint32_t w, uint32_t acc) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(w), "r"(0u), "r"(acc));
+    return r;
   }
 };
 template <>

@@ -4,12 +4,53 @@
 // For row t of sequence s in group g, with n_s rows in the call and j = t - row_start[s]:
 //   p_k = softmax_k(scale q . k) over the prefix's prefix_len[g] rows and the sequence's
 //   own rows 0 .. seq_len[s] - n_s + j,  out = sum_k p_k v_k.
+//
+// Unit of work: up to 256 query rows of a group that read the same key head (tokens x the
+// query heads of that key head), so that a prefix key is loaded once for all of them.
+// Its keys come in tiles of 128: first the prefix's, then the own rows of the unit's
+// sequences, packed in slots of 16 keys (a slot has one owner; a row masks the slots of
+// others), so short sequences share tiles and decoding needs no second kernel for them.
+//   plan kernel     counts each unit's tiles from the lengths in device memory;
+//   attend kernel   one CTA per SM takes an equal run of all units' tiles, wherever it
+//                   begins or ends: few units with long prefixes are split over the SMs;
+//   finish kernel   joins the pieces of split units by their maxima and sums, and computes
+//                   some rows again, key by key (see below).
+//
+// In the attend kernel two groups of four softmax warps work on alternate jobs.  Up to
+// 128 query rows, a job is a key tile, and the groups' outputs are joined at the unit's
+// end; above, both groups take every tile, each with its own 128 rows.  One warp walks
+// the schedule and loads (TMA), one issues tcgen05.mma (S = Q K^T, and O += P V with P
+// from TMEM), one loads the next unit's queries, one cleans value tiles.  S, P and O live
+// in TMEM.
+//
+// 0 x NaN is NaN, so a value that is no number spoils rows that give it no weight.  The
+// cleaning warp clears the value rows past a sequence's end, whatever the pages hold there,
+// and looks through tiles of own keys, which rows of other sequences (and earlier rows of
+// the same one) do not see: infinities and NaN there become 0 in the tile, and all rows of
+// the sequence that has them are computed again from their visible keys alone.  Nothing is
+// looked for in the prefix, which all rows see.
 #include <cmath>
+#include <mutex>
 
 #include "fe_ops.cuh"
 
 namespace fe {
 namespace {
+
+constexpr int kUnitRows = 256, kTileKeys = 128, kSlot = 16, kSlots = kTileKeys / kSlot;
+constexpr int kListed = 1 << 16;  // rows to compute again that the list holds
+constexpr int kDirty = 3, kUnitsAhead = 8;
+
+struct PlanHead {
+  int status;   // ST_ bits of this call
+  int bad;      // the row or group offsets are not what they must be: all rows NaN
+  int listed;   // rows to compute again (more than kListed: all rows are looked at)
+  int n_tiles;  // row tiles (units per key head)
+};
+// A split unit, by the CTA that has its first piece: rows and further pieces (0: none)
+struct SplitRec {
+  int pieces, t0, r0, rows, head, pad[3];
+};
 
 struct PrefixParams {
   const int32_t *group_start, *prefix_len, *prefix_pages, *row_start, *seq_len, *pages;
@@ -18,27 +59,961 @@ struct PrefixParams {
   float* lse;
   int32_t* status;
   int64_t q_row, q_head;
-  int n_groups, n_seqs, n_rows, hq, hkv, prefix_cols, page_cols, page_rows, n_pages;
-  float scale;
+  int n_groups, n_seqs, n_rows, hq, hkv, hr, prefix_cols, page_cols, page_rows, n_pages;
+  float scale, sc;  // sc: scale log2(e), and no 0 (masked scores, -inf, are multiplied by it)
+  int ctas, max_tiles;
+  // workspace
+  PlanHead* head;
+  int* gtile;          // [n_groups + 1] first row tile of a group
+  long long* gcost;    // [n_groups + 1] key tiles of all heads before a group
+  int* cost;           // [max_tiles] key tiles of a row tile (one head), at least 1
+  long long* before;   // [max_tiles + 1] key tiles of one head before a row tile
+  SplitRec* recs;      // [ctas]
+  int* list;           // [kListed]
+  float* part_o;       // [ctas][2][kUnitRows][D]
+  float2* part_ml;     // [ctas][2][kUnitRows] maximum (log2 units) and sum
 };
 
-// One warp per row and query head, 32 keys at a time.
-template <typename T, int D>
-__global__ void __launch_bounds__(128) prefix_simple_kernel(const PrefixParams p) {
-  __shared__ float sq[4][D];
+// The sequence's own rows that row j of its n sees, and whether its length is one
+__device__ __forceinline__ bool len_ok(const PrefixParams& p, int len) {
+  return len >= 0 && (long long)len <= (long long)p.page_cols * p.page_rows;
+}
+__device__ __forceinline__ bool prefix_ok(const PrefixParams& p, int n) {
+  return n >= 0 && (long long)n <= (long long)p.prefix_cols * p.page_rows;
+}
+__device__ __forceinline__ int seen_rows(int len, int n, int j) { return max(0, min(len, len - n + j + 1)); }
+
+// ---------------------------------------------------------------------------
+// plan
+// ---------------------------------------------------------------------------
+constexpr int kPlanThreads = 1024;
+
+// inclusive sum over the block's threads
+template <typename V>
+__device__ V block_scan(V v, V* sh) {
+  const int lane = threadIdx.x & 31, wp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const V u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  __syncthreads();
+  if (lane == 31) sh[wp] = v;
+  __syncthreads();
+  if (wp == 0) {
+    V w = sh[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const V u = __shfl_up_sync(0xffffffffu, w, o);
+      if (lane >= o) w += u;
+    }
+    sh[lane] = w;
+  }
+  __syncthreads();
+  return wp > 0 ? v + sh[wp - 1] : v;
+}
+
+// the largest i < n with a[i] <= x (a[0] <= x)
+template <typename V>
+__device__ __forceinline__ int find_last(const V* a, int n, V x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (a[mid] <= x)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) prefix_plan_kernel(const PrefixParams p) {
+  __shared__ long long sh[32];
+  __shared__ int sh_i[32];
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x & 31, wp = threadIdx.x >> 5;
-  const long long w = (long long)blockIdx.x * 4 + wp;
+  const int tid = threadIdx.x;
+  // offsets that are not increasing from 0 to their ends would send rows nowhere
+  bool bad = p.row_start[0] != 0 || p.row_start[p.n_seqs] != p.n_rows || p.group_start[0] != 0 ||
+             p.group_start[p.n_groups] != p.n_seqs;
+  for (int s = tid; s < p.n_seqs; s += kPlanThreads) bad |= p.row_start[s] > p.row_start[s + 1];
+  for (int g = tid; g < p.n_groups; g += kPlanThreads) bad |= p.group_start[g] > p.group_start[g + 1];
+  bad = __syncthreads_or(bad);
+  if (tid == 0) *p.head = PlanHead{0, bad ? 1 : 0, 0, 0};
+  if (bad) return;
+  // row tiles of the groups
+  int base = 0;
+  for (int g0 = 0; g0 < p.n_groups; g0 += kPlanThreads) {
+    const int g = g0 + tid;
+    int n = 0;
+    if (g < p.n_groups) {
+      const long long rows = (long long)(p.row_start[p.group_start[g + 1]] - p.row_start[p.group_start[g]]) * p.hr;
+      n = (int)((rows + kUnitRows - 1) / kUnitRows);
+    }
+    const int incl = block_scan(n, sh_i);
+    if (g < p.n_groups) p.gtile[g] = base + incl - n;
+    __syncthreads();
+    base += sh_i[31];
+    __syncthreads();
+  }
+  const int tiles = base;
+  if (tid == 0) {
+    p.gtile[p.n_groups] = tiles;
+    p.head->n_tiles = tiles;
+  }
+  for (int i = tid; i < tiles; i += kPlanThreads) p.cost[i] = 0;
+  __syncthreads();
+  // slots of own keys: a sequence's first row tile by the sequence, its further ones by the tile
+  auto slots = [&](int s, int a, int n, int first, int i) {  // sequence s (rows a .. of the group's first, n of them) in tile i
+    const int len = p.seq_len[s];
+    const int j = min(n - 1, (int)(((long long)(i + 1) * kUnitRows - 1) / p.hr) - (a - first));
+    return len_ok(p, len) ? (seen_rows(len, n, j) + kSlot - 1) / kSlot : 0;
+  };
+  for (int s = tid; s < p.n_seqs; s += kPlanThreads) {
+    const int a = p.row_start[s], n = p.row_start[s + 1] - a;
+    if (n == 0) continue;
+    const int g = find_last(p.group_start, p.n_groups, s), first = p.row_start[p.group_start[g]];
+    const int i = (int)((long long)(a - first) * p.hr / kUnitRows);
+    const int c = slots(s, a, n, first, i);
+    if (c) atomicAdd(p.cost + p.gtile[g] + i, c);
+  }
+  for (int rt = tid; rt < tiles; rt += kPlanThreads) {
+    const int g = find_last(p.gtile, p.n_groups, rt), i = rt - p.gtile[g];
+    if (i == 0) continue;
+    const int first = p.row_start[p.group_start[g]], t = first + (int)((long long)i * kUnitRows / p.hr);
+    const int s = find_last(p.row_start, p.n_seqs, t), a = p.row_start[s];
+    if ((long long)(a - first) * p.hr / kUnitRows < i) {
+      const int c = slots(s, a, p.row_start[s + 1] - a, first, i);
+      if (c) atomicAdd(p.cost + rt, c);
+    }
+  }
+  __syncthreads();
+  // key tiles of the row tiles, and those before them
+  long long run = 0;
+  for (int r0 = 0; r0 < tiles; r0 += kPlanThreads) {
+    const int rt = r0 + tid;
+    long long c = 0;
+    if (rt < tiles) {
+      const int g = find_last(p.gtile, p.n_groups, rt), n = p.prefix_len[g];
+      c = ((prefix_ok(p, n) ? n : 0) + kTileKeys - 1) / kTileKeys + (p.cost[rt] + kSlots - 1) / kSlots;
+      c = c < 1 ? 1 : c;
+      p.cost[rt] = (int)c;
+    }
+    const long long incl = block_scan(c, sh);
+    if (rt < tiles) p.before[rt] = run + incl - c;
+    __syncthreads();
+    run += sh[31];
+    __syncthreads();
+  }
+  if (tid == 0) p.before[tiles] = run;
+  __syncthreads();
+  for (int g = tid; g <= p.n_groups; g += kPlanThreads) p.gcost[g] = p.before[p.gtile[g]] * p.hkv;
+}
+
+// ---------------------------------------------------------------------------
+// attend
+// ---------------------------------------------------------------------------
+// What the loading warp tells the others about a key tile
+struct TileDesc {
+  int flags, slots, bad, clean, piece, entry, pad[2];
+  int owner[kSlots];  // sequence, or -1: the prefix
+  int base[kSlots];   // the slot's first key
+  int count[kSlots];  // its valid keys
+};
+enum : int { TD_FIRST = 1, TD_LAST = 2, TD_BOTH = 4, TD_FULL = 8, TD_END = 16, TD_SCAN = 32 };
+struct UnitInfo {
+  int t0, r0, rows, head, both, group, end, pad;
+};
+struct RowInfo {
+  int seq, seen, out, pad;  // sequence (-5: no row), own keys seen (-1: spoiled), row of the output
+};
+
+// Sequences with values that are no numbers, of one of the last kUnitsAhead units
+struct Dirty {
+  int n, seq[kDirty];  // n > kDirty: any of them
+};
+
+template <int D>
+struct PrefixCfg {
+  static constexpr int kThreads = 384;
+  static constexpr uint32_t kRow = D >= 64 ? 128 : 64;  // bytes of a swizzled row
+  static constexpr int NH = D == 128 ? 2 : 1;           // column halves of a tile
+  static constexpr uint32_t kHalf = 128 * kRow, kTile = NH * kHalf;
+  static constexpr int NK = D == 128 ? 2 : D == 64 ? 5 : 8, NV = NK;
+  static constexpr uint32_t kSwz = D >= 64 ? 2u : 4u;  // descriptor swizzle code (128 B / 64 B)
+  // TMEM columns: S of group w, P (its own columns where they fit), O
+  static constexpr bool kOwnP = D <= 64;
+  static constexpr uint32_t kS = 0, kP = kOwnP ? 256 : 0, kPStep = kOwnP ? 64 : 128, kO = kOwnP ? 384 : 256;
+  static_assert(kO + 2 * D <= 512, "TMEM budget");
+  static constexpr int ND = 6;  // tile descriptors in flight
+  static constexpr int kBars = 3 * NV + 2 * NK + 2 * ND + 2 * 4 + 2 * 3 + 16 + kUnitsAhead + 1;
+  static constexpr size_t kFixed = sizeof(TileDesc) * ND + sizeof(UnitInfo) * 2 + sizeof(RowInfo) * 256 +
+                                   sizeof(float2) * 256 + sizeof(Dirty) * kUnitsAhead + 8 * kBars + 16;
+  static_assert(ND < kUnitsAhead, "a unit's dirty sequences are read before the entry is used again");
+  static constexpr size_t kSmem = 1024 + (size_t)(2 + NK + NV) * kTile + kFixed;
+  static_assert(kSmem <= 232448, "shared memory budget");
+};
+
+__device__ __forceinline__ uint64_t tile_desc(uint32_t saddr, uint32_t lbo, uint32_t sbo, uint32_t swz) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(lbo >> 4) << 16;
+  d |= (uint64_t)(sbo >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)swz << 61;
+  return d;
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void mbar_arrive_lane0(uint64_t* bar) {
+  __syncwarp();
+  mbar_arrive_if_at(smem_u32(bar), (threadIdx.x & 31) == 0);
+}
+
+// A ring position: stage and the parity of its phase
+template <int N>
+struct Ring {
+  int i = 0;
+  uint32_t par = 0;
+  __device__ __forceinline__ void next() {
+    if (++i == N) {
+      i = 0;
+      par ^= 1u;
+    }
+  }
+};
+
+// maximum of 64 values, in four chains
+__device__ __forceinline__ float max64(const float* v) {
+  float a[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+  for (int i = 4; i + 8 <= 64; i += 8) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      asm("max.f32 %0, %1, %2, %3;" : "=f"(a[k]) : "f"(a[k]), "f"(v[i + 2 * k]), "f"(v[i + 2 * k + 1]));
+  }
+  a[0] = fmaxf(fmaxf(a[0], v[60]), v[61]);
+  a[1] = fmaxf(fmaxf(a[1], v[62]), v[63]);
+  return fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
+    prefix_attend_kernel(const __grid_constant__ CUtensorMap tK, const __grid_constant__ CUtensorMap tV,
+                         const PrefixParams p) {
+  using C = PrefixCfg<D>;
+  constexpr int NK = C::NK, NV = C::NV, ND = C::ND;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint8_t* sQ = smem;                    // [2] halves of 128 rows
+  uint8_t* sK = sQ + 2 * C::kTile;       // [NK]
+  uint8_t* sV = sK + NK * C::kTile;      // [NV]
+  TileDesc* descs = reinterpret_cast<TileDesc*>(sV + NV * C::kTile);
+  UnitInfo* units = reinterpret_cast<UnitInfo*>(descs + ND);
+  RowInfo* rinfo = reinterpret_cast<RowInfo*>(units + 2);       // [2][128]
+  float2* s_ml = reinterpret_cast<float2*>(rinfo + 256);        // [2][128]
+  Dirty* dirty = reinterpret_cast<Dirty*>(s_ml + 256);          // [kUnitsAhead]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(dirty + kUnitsAhead);
+  uint64_t *k_full = bars, *k_empty = k_full + NK;
+  uint64_t *v_full = k_empty + NK, *v_ready = v_full + NV, *v_empty = v_ready + NV;
+  uint64_t *d_full = v_empty + NV, *d_empty = d_full + ND;
+  uint64_t *s_full = d_empty + ND, *p_full = s_full + 2, *pv_done = p_full + 2;  // [2] by softmax group
+  uint64_t *u_full = pv_done + 2, *u_empty = u_full + 2, *q_full = u_empty + 2, *q_free = q_full + 2;  // [2]
+  uint64_t *x_full = q_free + 2, *x_read = x_full + 8;  // [2][4] exchange between the groups' warps
+  uint64_t *cleaned = x_read + 8, *drain = cleaned + kUnitsAhead;  // [kUnitsAhead] a unit's values are clean
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::kBars; ++i) mbar_init(bars + i, 1);
+    for (int i = 0; i < ND; ++i) mbar_init(d_empty + i, 10);  // 8 softmax warps, the issuer, the cleaner
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(p_full + i, 4);
+      mbar_init(q_free + i, 8);
+    }
+    fence_mbar_init();
+    prefetch_tmap(&tK);
+    prefetch_tmap(&tV);
+  }
+  if (warp == 1) tmem_alloc(tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  pdl_trigger();
+  pdl_wait();
+  int* status = &p.head->status;
+
+  if (warp < 4) {
+    if (warp == 0) {
+      // ---------------- schedule and loads ----------------
+      const int cta = blockIdx.x;
+      const bool bad_plan = p.head->bad != 0;
+      const long long total = bad_plan ? 0 : p.gcost[p.n_groups];
+      // (no more CTAs than tiles: each of them has one at least)
+      const int ctas = (int)min((long long)p.ctas, total);
+      const long long hi = cta < ctas ? total * (cta + 1) / ctas : 0;
+      long long x = cta < ctas ? total * cta / ctas : 0;
+      Ring<NK> kr;
+      Ring<NV> vr;
+      Ring<ND> dr;
+      Ring<2> ur;
+      bool ok = true;
+      SplitRec rec = {};
+      while (ok && x < hi) {
+        // the unit that holds tile x: group, head, row tile
+        const int g = find_last(p.gcost, p.n_groups + 1, x);
+        // (groups without rows have no tiles: the last of equal starts is the one with some)
+        const int first_rt = p.gtile[g], n_rt = p.gtile[g + 1] - first_rt;
+        const long long per_head = (p.gcost[g + 1] - p.gcost[g]) / p.hkv, rem = x - p.gcost[g];
+        const int head = (int)(rem / per_head);
+        const long long y = rem - (long long)head * per_head + p.before[first_rt];
+        const int ti = find_last(p.before + first_rt, n_rt, y), rt = first_rt + ti;
+        const int cost = p.cost[rt], off = (int)(y - p.before[rt]);
+        const int n = (int)min((long long)(cost - off), hi - x);
+        const int s0 = p.group_start[g], s1 = p.group_start[g + 1], t0 = p.row_start[s0];
+        const int r0 = ti * kUnitRows, rows = (int)min((long long)kUnitRows, (long long)(p.row_start[s1] - t0) * p.hr - r0);
+        const int both = rows > 128;
+        const int piece = off == 0 && n == cost ? -1 : off == 0 ? 1 : 0;
+        if (piece == 1) {  // further pieces: the CTAs that begin inside the unit
+          const long long end = x + cost;
+          int c = cta + 1;
+          while (c < ctas && total * c / ctas < end) ++c;
+          rec = SplitRec{c - cta - 1, t0, r0, rows, head, {}};
+        }
+        // tell the query loader
+        if (!(ok = mbar_wait_ok(u_empty + ur.i, ur.par ^ 1u, status))) break;
+        if (lane == 0) units[ur.i] = UnitInfo{t0, r0, rows, head, both, g, 0, 0};
+        mbar_arrive_lane0(u_full + ur.i);
+        const int entry = ur.i;
+        ur.next();
+        const int plen = prefix_ok(p, p.prefix_len[g]) ? p.prefix_len[g] : 0;
+        const int ptiles = (plen + kTileKeys - 1) / kTileKeys;
+        // own keys: the sequences of the unit's rows, 32 at a time, with their first slots
+        const int ta = t0 + r0 / p.hr, tb = t0 + (r0 + rows - 1) / p.hr;
+        int cs = 0, c_seen = 0, c_start = 0, c_end = 0;  // chunk's first sequence; lane's keys, first slot; the chunk's end
+        bool own_open = false;
+        auto chunk = [&](int from, int start) {
+          cs = from;
+          const int s = from + lane;
+          int slots = 0;
+          c_seen = 0;
+          if (s < s1) {
+            const int a = p.row_start[s], m = p.row_start[s + 1] - a, len = p.seq_len[s];
+            if (m > 0 && a <= tb && a + m > ta && len_ok(p, len)) c_seen = seen_rows(len, m, min(m - 1, tb - a));
+          }
+          slots = (c_seen + kSlot - 1) / kSlot;
+          int incl = slots;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += u;
+          }
+          c_start = start + incl - slots;
+          c_end = start + __shfl_sync(0xffffffffu, incl, 31);
+        };
+        // a batch of 32 slots (four tiles) of one part; this lane's slot
+        int b_first = -1, b_part = -1;  // first tile of the batch, its part
+        int b_owner = 0, b_base = 0, b_count = 0, b_row = 0, b_bad = 0;
+        auto batch = [&](int tile, int part) {
+          b_first = tile;
+          b_part = part;
+          b_owner = -2;
+          b_base = b_count = b_row = b_bad = 0;
+          const int32_t* table = nullptr;
+          int cols = 0;
+          if (part == 0) {
+            const int k = (tile * kSlots + lane) * kSlot;
+            if (k < plen) {
+              b_owner = -1;
+              b_base = k;
+              b_count = min(kSlot, plen - k);
+              table = p.prefix_pages + (long long)g * p.prefix_cols;
+              cols = p.prefix_cols;
+            }
+          } else {
+            const int slot = (tile - ptiles) * kSlots + lane;
+            if (!own_open) {
+              own_open = true;
+              const int f = s0 + warp_find_row(p.row_start + s0, s1 - s0, ta);
+              chunk(f, 0);
+            }
+            while (true) {
+              // the chunk's sequence with the last first slot at or before this lane's (empty ones lie before it)
+              int at = 0;
+#pragma unroll
+              for (int o = 16; o > 0; o >>= 1) {
+                const int st = __shfl_sync(0xffffffffu, c_start, min(at + o, 31));
+                if (at + o < 32 && st <= slot) at += o;
+              }
+              const int st = __shfl_sync(0xffffffffu, c_start, at), seen = __shfl_sync(0xffffffffu, c_seen, at);
+              if (b_owner == -2 && slot < c_end && slot >= st && (slot - st) * kSlot < seen) {
+                b_owner = cs + at;
+                b_base = (slot - st) * kSlot;
+                b_count = min(kSlot, seen - b_base);
+                table = p.pages + (long long)b_owner * p.page_cols;
+                cols = p.page_cols;
+              }
+              // past the chunk's end: the next one, as long as its sequences have rows here
+              if (!__any_sync(0xffffffffu, b_owner == -2 && slot >= c_end) || cs + 32 >= s1 || p.row_start[cs + 32] > tb) break;
+              chunk(cs + 32, c_end);
+            }
+          }
+          if (table) {
+            const int col = b_base / p.page_rows;
+            int page = col < cols ? __ldg(table + col) : -1;
+            if (page < 0 || page >= p.n_pages) {
+              b_bad = 1;
+              page = 0;
+            }
+            b_row = (page * p.hkv + head) * p.page_rows + (b_base - col * p.page_rows);
+          }
+        };
+        for (int j = off; j < off + n; ++j, ++x) {
+          const int part = j >= ptiles;
+          if (b_part != part || j >= b_first + 4) batch(j, part);
+          const int l0 = (j - b_first) * kSlots;  // the tile's first lane
+          const bool mine = lane >= l0 && lane < l0 + kSlots;
+          // (a tile of the prefix ends with it, whatever the batch goes on with)
+          const uint32_t used = __ballot_sync(0xffffffffu, mine && b_owner != -2);
+          const uint32_t badm = __ballot_sync(0xffffffffu, mine && b_bad), part_m = __ballot_sync(0xffffffffu, mine && b_owner != -2 && b_count < kSlot);
+          const int slots = __popc(used);
+          if (!(ok = mbar_wait_ok(d_empty + dr.i, dr.par ^ 1u, status))) break;
+          TileDesc* td = descs + dr.i;
+          if (mine) {
+            td->owner[lane - l0] = b_owner;
+            td->base[lane - l0] = b_base;
+            td->count[lane - l0] = b_count;
+          }
+          if (lane == 0) {
+            td->flags = (j == off ? TD_FIRST : 0) | (j == off + n - 1 ? TD_LAST : 0) | (both ? TD_BOTH : 0) |
+                        (part == 0 && slots == kSlots && part_m == 0 && badm == 0 ? TD_FULL : 0) |
+                        (part == 1 && ta != tb ? TD_SCAN : 0);
+            td->slots = slots;
+            td->bad = (int)(badm >> l0);
+            td->clean = (int)(part_m >> l0);
+            td->piece = piece;
+            td->entry = entry;
+          }
+          mbar_arrive_lane0(d_full + dr.i);
+          dr.next();
+          if (slots == 0) continue;
+          const uint32_t bytes = (uint32_t)slots * kSlot * D * 2;
+          const uint32_t go = mine && b_owner != -2;
+          if (!(ok = mbar_wait_ok(k_empty + kr.i, kr.par ^ 1u, status))) break;
+          mbar_arrive_expect_tx_if(k_full + kr.i, bytes, lane == 0);
+          __syncwarp();
+#pragma unroll
+          for (int hf = 0; hf < C::NH; ++hf)
+            tma_load_2d_if(sK + kr.i * C::kTile + hf * C::kHalf + (lane - l0) * kSlot * C::kRow, &tK, 64 * hf, b_row,
+                           k_full + kr.i, go);
+          kr.next();
+          if (!(ok = mbar_wait_ok(v_empty + vr.i, vr.par ^ 1u, status))) break;
+          mbar_arrive_expect_tx_if(v_full + vr.i, bytes, lane == 0);
+          __syncwarp();
+#pragma unroll
+          for (int hf = 0; hf < C::NH; ++hf)
+            tma_load_2d_if(sV + vr.i * C::kTile + hf * C::kHalf + (lane - l0) * kSlot * C::kRow, &tV, 64 * hf, b_row,
+                           v_full + vr.i, go);
+          vr.next();
+        }
+      }
+      if (ok && mbar_wait_ok(d_empty + dr.i, dr.par ^ 1u, status)) {
+        if (lane == 0) descs[dr.i].flags = TD_END;
+        mbar_arrive_lane0(d_full + dr.i);
+        if (mbar_wait_ok(u_empty + ur.i, ur.par ^ 1u, status)) {
+          if (lane == 0) units[ur.i].end = 1;
+          mbar_arrive_lane0(u_full + ur.i);
+        }
+      }
+      if (lane == 0) p.recs[cta] = rec;
+      // the loads land before the shared memory goes away, whatever became of their readers
+      mbar_landed_ring(k_full, kr.i, kr.par ^ 1u, NK, status);
+      mbar_landed_ring(v_full, vr.i, vr.par ^ 1u, NV, status);
+    } else if (warp == 1) {
+      // ---------------- products ----------------
+      const uint32_t go = elect_one();
+      constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u;
+      const uint32_t idesc = (1u << 4) | kType | (8u << 24);
+      const uint32_t idesc_pv = idesc | (1u << 16) | ((uint32_t)(D >> 3) << 17);  // V is MN-major
+      const uint64_t qd0 = tile_desc(smem_u32(sQ), 16, 8 * C::kRow, C::kSwz);
+      const uint64_t kd0 = tile_desc(smem_u32(sK), 16, 8 * C::kRow, C::kSwz);
+      const uint64_t vd0 = tile_desc(smem_u32(sV), C::kHalf, 8 * C::kRow, C::kSwz);
+      Ring<NK> kr;
+      Ring<NV> vr;
+      Ring<ND> dr;
+      uint32_t qpar[2] = {0, 0};
+      // jobs whose product with V is still to come, oldest first
+      struct Job {
+        int w, slots, first, release, vi;
+        uint32_t vpar;
+      } q[2];
+      int pending = 0;
+      uint32_t jobs[2] = {0, 0};  // finished jobs of a group
+      bool opened[2] = {false, false};
+      int jp = 0;
+      bool ok = true;
+      auto finish = [&]() {  // O += P V of the oldest job
+        const Job& b = q[0];
+        const int w = b.w;
+        if (!mbar_wait_ok(p_full + w, jobs[w] & 1u, status) || !mbar_wait_ok(v_ready + b.vi, b.vpar, status)) return false;
+        tc_fence_after();
+        const uint32_t o = tmem + C::kO + (uint32_t)(w * D), a = tmem + C::kP + (uint32_t)w * C::kPStep;
+        const uint64_t vd = vd0 + (uint64_t)((b.vi * C::kTile) >> 4);
+        for (int s = 0; s < b.slots; ++s)
+          umma_bf16_tmem_a_if(o, a + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv,
+                              s != 0 || !b.first ? 1u : 0u, go);
+        umma_commit_if(pv_done + w, go);
+        if (b.release) umma_commit_if(v_empty + b.vi, go);
+        ++jobs[w];
+        q[0] = q[1];
+        --pending;
+        return true;
+      };
+      // What the next job needs may itself wait for a pending one (its queries' space, a stage of V): as long as
+      // it is not there, pending jobs are finished.
+      auto ready = [&](uint64_t* bar, uint32_t par) {
+        while (pending > 0 && !__all_sync(0xffffffffu, mbar_test_wait(bar, par)))
+          if (!finish()) return false;
+        return mbar_wait_ok(bar, par, status);
+      };
+      while (ok) {
+        if (!(ok = ready(d_full + dr.i, dr.par))) break;
+        const TileDesc* td = descs + dr.i;
+        const int flags = td->flags, slots = td->slots, entry = td->entry;
+        if (flags & TD_END) break;
+        mbar_arrive_lane0(d_empty + dr.i);
+        dr.next();
+        const bool both = flags & TD_BOTH;
+        if (flags & TD_FIRST) {
+          if (!(ok = ready(q_full + entry, qpar[entry]))) break;
+          qpar[entry] ^= 1u;
+          opened[0] = opened[1] = false;
+        }
+        if (slots == 0) continue;
+        if (!(ok = ready(k_full + kr.i, kr.par))) break;
+        const uint64_t kd = kd0 + (uint64_t)((kr.i * C::kTile) >> 4);
+        const uint32_t id = idesc | ((uint32_t)(slots * 2) << 17);
+        for (int e = 0; e < (both ? 2 : 1); ++e) {
+          const int w = jp;
+          jp ^= 1;
+          if (pending == 2 && !(ok = finish())) break;
+          // (without columns of its own, P lies where the next S goes)
+          if (!C::kOwnP && jobs[w] > 0 && !(ok = mbar_wait_ok(pv_done + w, (jobs[w] - 1) & 1u, status))) break;
+          tc_fence_after();
+          const uint64_t qd = qd0 + (uint64_t)(((both ? w : entry) * C::kTile) >> 4);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint64_t at = (uint64_t)(((kk * 32) / C::kRow * C::kHalf + (kk * 32) % C::kRow) >> 4);
+            umma_bf16_if(tmem + C::kS + (uint32_t)(w * 128), qd + at, kd + at, id, kk != 0 ? 1u : 0u, go);
+          }
+          umma_commit_if(s_full + w, go);
+          const bool last = !both || e == 1;
+          if (last) umma_commit_if(k_empty + kr.i, go);
+          q[pending++] = Job{w, slots, !opened[w], last, vr.i, vr.par};
+          opened[w] = true;
+        }
+        if (!ok) break;
+        kr.next();
+        vr.next();
+      }
+      while (ok && pending > 0) ok = finish();
+      umma_drain(drain, status, go);
+    } else if (warp == 2) {
+      // ---------------- values ----------------
+      Ring<NV> vr;
+      Ring<ND> dr;
+      uint32_t unit = 0;
+      while (true) {
+        if (!mbar_wait_ok(d_full + dr.i, dr.par, status)) break;
+        const TileDesc* td = descs + dr.i;
+        const int flags = td->flags, slots = td->slots, clean = td->clean;
+        const int count = lane < kSlots ? td->count[lane] : 0, owner = lane < kSlots ? td->owner[lane] : -1;
+        if (flags & TD_END) break;
+        mbar_arrive_lane0(d_empty + dr.i);
+        dr.next();
+        Dirty* dt = dirty + unit % kUnitsAhead;
+        if ((flags & TD_FIRST) && lane == 0) dt->n = 0;
+        if (slots > 0) {
+          if (!mbar_wait_ok(v_full + vr.i, vr.par, status)) break;
+          uint8_t* v = sV + vr.i * C::kTile;
+          if (clean) {
+            for (int s = 0; s < slots; ++s) {
+              const int n = __shfl_sync(0xffffffffu, count, s);
+              // (whole rows: the swizzle moves pieces within a row)
+              for (int hf = 0; hf < C::NH; ++hf)
+                for (uint32_t o = (uint32_t)n * C::kRow + lane * 16; o < kSlot * C::kRow; o += 512)
+                  *reinterpret_cast<uint4*>(v + hf * C::kHalf + s * kSlot * C::kRow + o) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            __syncwarp();
+          }
+          if (flags & TD_SCAN) {
+            // 0 x as long as every x is a number, NaN from the first other one on
+            uint32_t acc = 0;
+            for (int hf = 0; hf < C::NH; ++hf)
+#pragma unroll 4
+              for (uint32_t o = lane * 16; o < (uint32_t)slots * kSlot * C::kRow; o += 512) {
+                const uint4 x = *reinterpret_cast<const uint4*>(v + hf * C::kHalf + o);
+                acc = Elem<T>::zero_fma(x.x, Elem<T>::zero_fma(x.y, Elem<T>::zero_fma(x.z, Elem<T>::zero_fma(x.w, acc))));
+              }
+            if (__any_sync(0xffffffffu, (acc & 0x7fff7fffu) != 0)) {
+              for (int s = 0; s < slots; ++s) {
+                bool found = false;
+                for (int hf = 0; hf < C::NH; ++hf)
+                  for (uint32_t o = lane * 2; o < kSlot * C::kRow; o += 64) {
+                    T* x = reinterpret_cast<T*>(v + hf * C::kHalf + s * kSlot * C::kRow + o);
+                    const float f = Elem<T>::get(*x) * 0.f;
+                    if (!(f == 0.f)) {
+                      found = true;
+                      *x = Elem<T>::put(0.f);
+                    }
+                  }
+                found = __any_sync(0xffffffffu, found);
+                const int who = __shfl_sync(0xffffffffu, owner, s);
+                if (found && lane == 0) {
+                  const int n = dt->n;
+                  if (n == 0 || n > kDirty || dt->seq[n - 1] != who) {
+                    if (n < kDirty) dt->seq[n] = who;
+                    dt->n = n + 1;
+                  }
+                }
+              }
+            }
+          }
+          fence_async_shared();
+          mbar_arrive_lane0(v_ready + vr.i);
+          vr.next();
+        }
+        if (flags & TD_LAST) {
+          mbar_arrive_lane0(cleaned + unit % kUnitsAhead);
+          ++unit;
+        }
+      }
+    } else {
+      // ---------------- queries ----------------
+      Ring<2> ur;
+      uint32_t uses[2] = {0, 0};
+      while (true) {
+        if (!mbar_wait_ok(u_full + ur.i, ur.par, status)) break;
+        const UnitInfo u = units[ur.i];
+        if (u.end) break;
+        const int e = ur.i;
+        mbar_arrive_lane0(u_empty + e);
+        ur.next();
+        bool ok = true;
+        const int h0 = u.both ? 0 : e, h1 = u.both ? 1 : e;
+        for (int h = h0; h <= h1 && ok; ++h) {
+          if (uses[h] > 0) ok = mbar_wait_ok(q_free + h, (uses[h] - 1) & 1u, status);
+          ++uses[h];
+        }
+        if (!ok) break;
+        const int s0 = p.group_start[u.group], s1 = p.group_start[u.group + 1];
+        const bool pre_ok = prefix_ok(p, p.prefix_len[u.group]);
+        const int n = u.both ? 256 : 128;
+        // the queries: pieces of 16 bytes, swizzled as TMA would have it
+        constexpr int NP = D / 8, RP = 32 / NP;  // pieces of a row, rows of a step
+        const int pc = lane % NP;
+        const uint32_t hoff = (uint32_t)(pc * 16) / C::kRow * C::kHalf, poff = (uint32_t)(pc * 16) % C::kRow;
+        for (int r = lane / NP; r < u.rows; r += RP) {
+          const int rr = u.r0 + r, t = u.t0 + rr / p.hr, h = u.head * p.hr + rr % p.hr;
+          const T* src = reinterpret_cast<const T*>(p.q) + (long long)t * p.q_row + h * p.q_head + pc * 8;
+          const uint32_t row = (uint32_t)(r & 127);
+          const uint32_t mask = C::kRow == 128 ? (row & 7u) : ((row >> 1) & 3u);
+          cp_async16(smem_u32(sQ) + (uint32_t)((u.both ? r >> 7 : e) * C::kTile) + hoff + row * C::kRow + (poff ^ (mask << 4)), src);
+        }
+        for (int r = lane; r < n; r += 32) {
+          RowInfo ri = {-5, 0, -1, 0};
+          if (r < u.rows) {
+            const int rr = u.r0 + r, t = u.t0 + rr / p.hr;
+            const int s = s0 + find_last(p.row_start + s0, s1 - s0, t), a = p.row_start[s];
+            const int len = p.seq_len[s];
+            ri.seq = s;
+            ri.seen = pre_ok && len_ok(p, len) ? seen_rows(len, p.row_start[s + 1] - a, t - a) : -1;
+            ri.out = t * p.hq + u.head * p.hr + rr % p.hr;
+          }
+          rinfo[(u.both ? 0 : e * 128) + r] = ri;
+        }
+        cp_async_wait();
+        fence_async_shared();
+        mbar_arrive_lane0(q_full + e);
+      }
+      cp_async_wait();
+    }
+  } else {
+    // ---------------- softmax and output ----------------
+    const int w = (warp - 4) >> 2, qd = warp & 3, row = qd * 32 + lane;
+    const uint32_t tl = tmem + ((uint32_t)(qd * 32) << 16);
+    const uint32_t t_s = tl + C::kS + (uint32_t)(w * 128), t_p = tl + C::kP + (uint32_t)w * C::kPStep;
+    const uint32_t t_o = tl + C::kO + (uint32_t)(w * D);
+    const float sc = p.sc;
+    Ring<ND> dr;
+    uint32_t qpar[2] = {0, 0}, jobs = 0, xs = 0, xr = 0;
+    int jp = 0, mine = 0;  // jobs of this unit
+    uint32_t unit = 0;
+    RowInfo ri = {-5, 0, -1, 0};
+    float m = -INFINITY, l = 0.f;
+    bool spoiled = false, active = false;
+    while (true) {
+      if (!mbar_wait_ok(d_full + dr.i, dr.par, status)) break;
+      const TileDesc* td = descs + dr.i;
+      const int flags = td->flags, slots = td->slots;
+      if (flags & TD_END) break;
+      const bool both = flags & TD_BOTH;
+      const int entry = td->entry, piece = td->piece;
+      if (flags & TD_FIRST) {
+        if (!mbar_wait_ok(q_full + entry, qpar[entry], status)) break;
+        qpar[entry] ^= 1u;
+        ri = rinfo[(both ? w * 128 : entry * 128) + row];
+        active = __any_sync(0xffffffffu, ri.seq >= 0);
+        m = -INFINITY;
+        l = 0.f;
+        mine = 0;
+        spoiled = ri.seen < 0;
+      }
+      const bool job = slots > 0 && (both || jp == w);
+      if (slots > 0 && !both) jp ^= 1;
+      if (job) {
+        if (!mbar_wait_ok(s_full + w, jobs & 1u, status)) break;
+        if (active) {
+          tc_fence_after();
+          // The keys' second half gives its maximum first and is read again after the first half
+          // (which needs 64 registers, not 128; P's columns may be the first half's).
+          auto half = [&](int c0, float* v) {  // scores of keys c0 .. c0 + 63, unseen ones -inf
+            tmem_ld64(t_s + (uint32_t)c0, v);
+            if (flags & TD_FULL) return;
+            const int bad = td->bad;
+#pragma unroll
+            for (int z = 0; z < kSlots / 2; ++z) {
+              const int at = c0 / kSlot + z, owner = td->owner[at];
+              int n = owner == -1 ? td->count[at] : owner == ri.seq ? min(td->count[at], max(0, ri.seen - td->base[at])) : 0;
+              if (at >= slots) n = 0;
+              spoiled = spoiled || (n > 0 && ((bad >> at) & 1));
+              if (__any_sync(0xffffffffu, n < kSlot)) {
+#pragma unroll
+                for (int i = 0; i < kSlot; ++i)
+                  if (i >= n) v[z * kSlot + i] = -INFINITY;
+              }
+            }
+          };
+          float v[64];
+          half(64, v);
+          float mx = max64(v);
+          half(0, v);
+          mx = fmaxf(mx, max64(v)) * sc;
+          constexpr float kSlack = 8.f;
+          if (mine == 0) {
+            m = mx;
+          } else {
+            const bool up = mx > m + kSlack;
+            if (__any_sync(0xffffffffu, up)) {
+              // the accumulator, complete up to this group's last job, to the new maximum
+              if (!mbar_wait_ok(pv_done + w, (jobs - 1) & 1u, status)) break;
+              tc_fence_after();
+              const float f = up ? ex2_approx(m - mx) : 1.f;
+              if (up) m = mx;
+              l *= f;
+#pragma unroll 1
+              for (int c0 = 0; c0 < D; c0 += 8) {
+                uint32_t o[8];
+                tmem_ld8(t_o + (uint32_t)c0, o);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                tmem_st8_nowait(t_o + (uint32_t)c0, o);
+              }
+            }
+          }
+          if (C::kOwnP && jobs > 0) {  // P's columns are free once the last job's product has read them
+            if (!mbar_wait_ok(pv_done + w, (jobs - 1) & 1u, status)) break;
+            tc_fence_after();
+          }
+          const float ref = m == -INFINITY ? 0.f : m;
+          const uint64_t sc2 = f32x2_pack(sc, sc), nm2 = f32x2_pack(-ref, -ref);
+          uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            if (c0 == 64) half(64, v);
+            uint32_t pk[16];
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+              float e[4];
+              f32x2_unpack(f32x2_fma(f32x2_pack(v[c0 % 64 + i], v[c0 % 64 + i + 1]), sc2, nm2), e[0], e[1]);
+              f32x2_unpack(f32x2_fma(f32x2_pack(v[c0 % 64 + i + 2], v[c0 % 64 + i + 3]), sc2, nm2), e[2], e[3]);
+#pragma unroll
+              for (int z = 0; z < 4; ++z) e[z] = ex2_approx(e[z]);
+              uint64_t& acc = sum[(i >> 2) & 1];
+              acc = f32x2_add(acc, f32x2_add(f32x2_pack(e[0], e[2]), f32x2_pack(e[1], e[3])));
+              pk[i / 2] = Elem<T>::put2(e[0], e[1]);
+              pk[i / 2 + 1] = Elem<T>::put2(e[2], e[3]);
+            }
+            tmem_st16_nowait(t_p + (uint32_t)(c0 / 2), pk);
+          }
+          float a0, a1, a2, a3;
+          f32x2_unpack(sum[0], a0, a1);
+          f32x2_unpack(sum[1], a2, a3);
+          l += (a0 + a1) + (a2 + a3);
+          tmem_st_wait();
+          tc_fence_before();
+        }
+        mbar_arrive_lane0(p_full + w);
+        ++jobs;
+        ++mine;
+      }
+      mbar_arrive_lane0(d_empty + dr.i);
+      dr.next();
+      if (!(flags & TD_LAST)) continue;
+
+      // ---------------- the piece's output ----------------
+      if (!mbar_wait_ok(cleaned + unit % kUnitsAhead, (unit / kUnitsAhead) & 1u, status)) break;
+      {
+        const Dirty dt = dirty[unit % kUnitsAhead];
+        if (dt.n > 0) {
+          spoiled = spoiled || dt.n > kDirty;
+#pragma unroll
+          for (int i = 0; i < kDirty; ++i) spoiled = spoiled || (i < dt.n && dt.seq[i] == ri.seq);
+        }
+        ++unit;
+      }
+      if (spoiled) l = NAN;
+      if (mine > 0) {
+        if (!mbar_wait_ok(pv_done + w, (jobs - 1) & 1u, status)) break;
+        tc_fence_after();
+      }
+      float f = 1.f;  // of this group's accumulator
+      float ms = m, ls = l;
+      const int h = both ? 0 : entry;  // the half whose space the exchange takes
+      if (!both) {
+        s_ml[w * 128 + row] = make_float2(m, l);
+        mbar_arrive_lane0(x_full + w * 4 + qd);
+        if (!mbar_wait_ok(x_full + (1 - w) * 4 + qd, xr & 1u, status)) break;
+        ++xr;
+        const float2 o = s_ml[(1 - w) * 128 + row];
+        ms = fmaxf(m, o.x);
+        const float ref = ms == -INFINITY ? 0.f : ms;
+        f = ex2_approx(m - ref);
+        const float fo = ex2_approx(o.x - ref);
+        ls = w == 0 ? fmaf(l, f, o.y * fo) : fmaf(o.y, fo, l * f);
+      }
+      const bool store = ri.out >= 0;
+      const float inv = ls == 0.f ? 0.f : 1.f / ls;
+      T* out = reinterpret_cast<T*>(p.out) + (long long)ri.out * D;
+      const long long slot = ((long long)blockIdx.x * 2 + (piece == 1)) * kUnitRows + (both ? w * 128 : 0) + row;
+      // columns c0 .. c0 + N - 1 of the row, summed
+      auto put = [&](auto count, int c0, float* o) {
+        constexpr int N = decltype(count)::value;
+        if (piece < 0) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) o[i] *= inv;
+          if (store) {
+#pragma unroll
+            for (int i = 0; i < N; i += 8) *reinterpret_cast<uint4*>(out + c0 + i) = piece_put<T>(o + i);
+          }
+        } else if (store) {
+#pragma unroll
+          for (int i = 0; i < N; i += 8) st_sector(p.part_o + slot * D + c0 + i, o + i);
+        }
+      };
+      if (both) {
+#pragma unroll 1
+        for (int c0 = 0; c0 < D; c0 += 32) {
+          float o[32];
+          if (mine > 0) {
+            tmem_ld32(t_o + (uint32_t)c0, o);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = 0.f;
+          }
+          put(std::integral_constant<int, 32>(), c0, o);
+        }
+      } else {
+        // each group finishes half of the columns; the other half goes to its partner through the unit's query space
+        constexpr int N = D / 4;
+        float* xb = reinterpret_cast<float*>(sQ + h * C::kTile);  // [2][N][128]
+        auto load = [&](int c0, float* o) {
+          if (mine > 0) {
+#pragma unroll
+            for (int i = 0; i < N; i += 8) {
+              uint32_t r8[8];
+              tmem_ld8(t_o + (uint32_t)(c0 + i), r8);
+#pragma unroll
+              for (int z = 0; z < 8; ++z) o[i + z] = __uint_as_float(r8[z]) * f;
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[i] = 0.f;
+          }
+        };
+        bool ok = true;
+#pragma unroll 1
+        for (int r = 0; r < 2 && ok; ++r) {
+          float o[N];
+          load((1 - w) * (D / 2) + r * N, o);
+          if (r == 1) ok = mbar_wait_ok(x_read + w * 4 + qd, xs & 1u, status);
+          if (!ok) break;
+#pragma unroll
+          for (int i = 0; i < N; ++i) xb[(w * N + i) * 128 + row] = o[i];
+          mbar_arrive_lane0(x_full + w * 4 + qd);
+          load(w * (D / 2) + r * N, o);
+          ok = mbar_wait_ok(x_full + (1 - w) * 4 + qd, xr & 1u, status);
+          if (!ok) break;
+          ++xr;
+#pragma unroll
+          for (int i = 0; i < N; ++i) o[i] += xb[((1 - w) * N + i) * 128 + row];
+          if (r == 0) mbar_arrive_lane0(x_read + (1 - w) * 4 + qd);
+          put(std::integral_constant<int, N>(), w * (D / 2) + r * N, o);
+        }
+        if (!ok) break;
+        ++xs;
+      }
+      tc_fence_before();
+      if (store) {
+        if (piece < 0) {
+          if (both || w == 0) {
+            if (!(ls == ls)) {
+              const int at = atomicAdd(&p.head->listed, 1);
+              if (at < kListed) p.list[at] = ri.out;
+            }
+            if (p.lse) p.lse[ri.out] = ls == 0.f ? -INFINITY : (ms + log2f(ls)) * 0.693147180559945309f;
+          }
+        } else if (both || w == 0) {
+          p.part_ml[slot] = make_float2(ms, ls);
+        }
+      }
+      fence_async_shared();
+      // this group is done with the unit's queries, row data and exchange space
+      __syncwarp();
+      if (both) {
+        mbar_arrive_if_at(smem_u32(q_free), lane == 0);
+        mbar_arrive_if_at(smem_u32(q_free + 1), lane == 0);
+      } else {
+        mbar_arrive_if_at(smem_u32(q_free + entry), lane == 0);
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// ---------------------------------------------------------------------------
+// finish
+// ---------------------------------------------------------------------------
+// A row from its visible keys alone, 32 at a time, by one warp (sq: its D queries)
+template <typename T, int D>
+__device__ void row_by_keys(const PrefixParams& p, long long w, float* sq) {
+  const int lane = threadIdx.x & 31;
   const int t = (int)(w / p.hq), h = (int)(w % p.hq), hk = h / (p.hq / p.hkv);
-  if (t >= p.n_rows) return;
   const int s = warp_find_row(p.row_start, p.n_seqs, t), g = warp_find_row(p.group_start, p.n_groups, s);
   const int r0 = p.row_start[s], n = p.row_start[s + 1] - r0, len = p.seq_len[s], np = p.prefix_len[g];
   bool bad = t < r0 || t >= r0 + n || s < p.group_start[g] || s >= p.group_start[g + 1] || len < 0 || np < 0 ||
              (long long)len > (long long)p.page_cols * p.page_rows || (long long)np > (long long)p.prefix_cols * p.page_rows;
   const int own = bad ? 0 : max(0, min(len, len - n + (t - r0) + 1)), pre = bad ? 0 : np;
+  __syncwarp();  // (an earlier row of this warp has been read)
   const T* q = reinterpret_cast<const T*>(p.q) + (long long)t * p.q_row + h * p.q_head;
-  for (int i = lane; i < D; i += 32) sq[wp][i] = Elem<T>::get(q[i]);
+  for (int i = lane; i < D; i += 32) sq[i] = Elem<T>::get(q[i]);
   __syncwarp();
   float m = -INFINITY, l = 0.f, o[D / 32] = {};
   for (int part = 0; part < 2; ++part) {
@@ -56,7 +1031,7 @@ __global__ void __launch_bounds__(128) prefix_simple_kernel(const PrefixParams p
           row = ((long long)page * p.hkv + hk) * p.page_rows + k % p.page_rows;
           const T* kr = reinterpret_cast<const T*>(p.k) + row * D;
           float a = 0.f;
-          for (int i = 0; i < D; ++i) a += sq[wp][i] * Elem<T>::get(kr[i]);
+          for (int i = 0; i < D; ++i) a += sq[i] * Elem<T>::get(kr[i]);
           x = a * p.scale;
         }
       }
@@ -91,6 +1066,71 @@ __global__ void __launch_bounds__(128) prefix_simple_kernel(const PrefixParams p
   if (p.lse && lane == 0) p.lse[w] = bad ? NAN : l == 0.f ? -INFINITY : m + logf(l);
 }
 
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) prefix_finish_kernel(const PrefixParams p) {
+  __shared__ float sq[8][D];
+  pdl_trigger();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, wp = threadIdx.x >> 5;
+  const long long rows = (long long)p.n_rows * p.hq;
+  const long long w0 = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 8 + wp, nw = (long long)gridDim.x * gridDim.y * 8;
+  if (p.head->bad) {
+    for (long long w = w0; w < rows; w += nw) {
+      T* out = reinterpret_cast<T*>(p.out) + w * D;
+      for (int i = lane; i < D; i += 32) out[i] = Elem<T>::put(NAN);
+      if (p.lse && lane == 0) p.lse[w] = NAN;
+    }
+    if (w0 == 0 && lane == 0 && p.status) atomicOr(p.status, FE_ST_INDEX);
+    return;
+  }
+  if (w0 == 0 && lane == 0 && p.status && p.head->status) atomicOr(p.status, p.head->status);
+  // the pieces of the unit that CTA blockIdx.x has the first one of
+  const SplitRec rec = p.recs[blockIdx.x];
+  if (rec.pieces > 0) {
+    constexpr int N = D / 32;
+    const long long first = (long long)blockIdx.x * 2 + 1;
+    auto slot = [&](int i, int r) { return (i == 0 ? first : 2LL * (blockIdx.x + i)) * kUnitRows + r; };
+    for (int r = blockIdx.y * 8 + wp; r < rec.rows; r += gridDim.y * 8) {
+      float m = -INFINITY;
+      for (int i = 0; i <= rec.pieces; ++i) m = fmaxf(m, p.part_ml[slot(i, r)].x);
+      const float ref = m == -INFINITY ? 0.f : m;
+      float l = 0.f, o[N] = {};
+      for (int i = 0; i <= rec.pieces; ++i) {
+        const float2 ml = p.part_ml[slot(i, r)];
+        const float f = ex2_approx(ml.x - ref);
+        l = fmaf(ml.y, f, l);
+        const float* po = p.part_o + slot(i, r) * D + lane * N;
+#pragma unroll
+        for (int z = 0; z < N; ++z) o[z] = fmaf(po[z], f, o[z]);
+      }
+      const int rr = rec.r0 + r;
+      const long long w = (long long)(rec.t0 + rr / p.hr) * p.hq + rec.head * p.hr + rr % p.hr;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+      for (int z = 0; z < N; ++z) o[z] *= inv;
+      if (!(l == l)) {
+        row_by_keys<T, D>(p, w, sq[wp]);
+        continue;
+      }
+      T* out = reinterpret_cast<T*>(p.out) + w * D + lane * N;
+#pragma unroll
+      for (int z = 0; z < N; ++z) out[z] = Elem<T>::put(o[z]);
+      if (p.lse && lane == 0) p.lse[w] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
+    }
+  }
+  const int listed = p.head->listed;
+  if (listed <= kListed) {
+    for (long long i = w0; i < listed; i += nw) row_by_keys<T, D>(p, p.list[i], sq[wp]);
+  } else {
+    for (long long w = w0; w < rows; w += nw) {
+      const T* out = reinterpret_cast<const T*>(p.out) + w * D;
+      float check = 0.f;
+      for (int i = lane; i < D; i += 32) check = fmaf(Elem<T>::get(out[i]), 0.f, check);
+      if (__any_sync(0xffffffffu, !(check == 0.f))) row_by_keys<T, D>(p, w, sq[wp]);
+    }
+  }
+}
 int check_prefix(const fe_prefix_args* a) {
   if (!a) return fail(FE_ERR_INVALID_ARG, "null arguments");
   const int rc = check_paged_kv(a->kv);
@@ -111,20 +1151,103 @@ int check_prefix(const fe_prefix_args* a) {
   return FE_OK;
 }
 
+
+// Sizes of the workspace's parts, in order, each on a 256-byte boundary
+struct Layout {
+  size_t head, gtile, gcost, cost, before, recs, list, part_o, part_ml, bytes;
+};
+Layout layout(const fe_prefix_args* a, int ctas, int max_tiles) {
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t x = at;
+    at += (n + 255) / 256 * 256;
+    return x;
+  };
+  Layout w;
+  w.head = take(sizeof(PlanHead));
+  w.gtile = take(4 * ((size_t)a->n_groups + 1));
+  w.gcost = take(8 * ((size_t)a->n_groups + 1));
+  w.cost = take(4 * (size_t)max_tiles);
+  w.before = take(8 * ((size_t)max_tiles + 1));
+  w.recs = take(sizeof(SplitRec) * ctas);
+  w.list = take(4 * (size_t)kListed);
+  w.part_o = take((size_t)ctas * 2 * kUnitRows * a->kv.head_dim * 4);
+  w.part_ml = take((size_t)ctas * 2 * kUnitRows * 8);
+  w.bytes = at;
+  return w;
+}
+
+// Row tiles at most: the groups' rows in whole tiles, and a part of one for each
+int most_tiles(const fe_prefix_args* a) {
+  return (int)((long long)a->n_rows * (a->q_heads / a->kv.kv_heads) / kUnitRows) + a->n_groups;
+}
+
+struct Device {
+  int sms = 0;
+  cudaError_t err = cudaErrorUnknown;
+};
+constexpr int kMaxDevices = 64;
+
+// Once per device: its SMs and the kernels' shared-memory limits.
+template <typename T, int D>
+cudaError_t allow_smem() {
+  return cudaFuncSetAttribute((const void*)prefix_attend_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)PrefixCfg<D>::kSmem);
+}
+const Device& device() {
+  static Device devs[kMaxDevices];
+  static std::once_flag once[kMaxDevices];
+  static const Device none;
+  int d = 0;
+  if (cudaGetDevice(&d) != cudaSuccess || d < 0 || d >= kMaxDevices) return none;
+  std::call_once(once[d], [d] {
+    Device& v = devs[d];
+    v.err = cudaDeviceGetAttribute(&v.sms, cudaDevAttrMultiProcessorCount, d);
+    for (cudaError_t (*f)() : {allow_smem<__nv_bfloat16, 32>, allow_smem<__nv_bfloat16, 64>, allow_smem<__nv_bfloat16, 128>,
+                               allow_smem<__half, 32>, allow_smem<__half, 64>, allow_smem<__half, 128>})
+      if (v.err == cudaSuccess) v.err = f();
+  });
+  return devs[d];
+}
+
+// [n_pages * kv_heads * page_rows, head_dim] in boxes of 16 rows by 128 (or 64) bytes
+bool encode_pages(CUtensorMap* m, const fe_paged_kv& kv, const void* base) {
+  const cuuint64_t dims[2] = {(cuuint64_t)kv.head_dim, (cuuint64_t)kv.n_pages * kv.kv_heads * kv.page_rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)kv.head_dim * 2};
+  const cuuint32_t box[2] = {(cuuint32_t)(kv.head_dim < 64 ? kv.head_dim : 64), (cuuint32_t)kSlot}, es[2] = {1u, 1u};
+  const EncodeTiledFn fn = encode_tiled_fn();
+  return fn && fn(m, kv.dtype == FE_IO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                  const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  kv.head_dim < 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int D>
+cudaError_t prefix_go(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, cudaStream_t s) {
+  using C = PrefixCfg<D>;
+  cudaError_t e = launch_k(prefix_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
+  if (e == cudaSuccess)
+    e = launch_k(prefix_attend_kernel<T, D>, dim3((unsigned)p.ctas), dim3(C::kThreads), C::kSmem, s, tk, tv, p);
+  if (e == cudaSuccess) e = launch_k(prefix_finish_kernel<T, D>, dim3((unsigned)p.ctas, 8), dim3(256), 0, s, p);
+  return e;
+}
 template <typename T>
-cudaError_t prefix_dim(const PrefixParams& p, int d, cudaStream_t s) {
-  const long long warps = (long long)p.n_rows * p.hq;
-  const dim3 g((unsigned)((warps + 3) / 4)), b(128);
-  return d == 32   ? launch_k(prefix_simple_kernel<T, 32>, g, b, 0, s, p)
-         : d == 64 ? launch_k(prefix_simple_kernel<T, 64>, g, b, 0, s, p)
-                   : launch_k(prefix_simple_kernel<T, 128>, g, b, 0, s, p);
+cudaError_t prefix_dim(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, int d, cudaStream_t s) {
+  return d == 32 ? prefix_go<T, 32>(tk, tv, p, s) : d == 64 ? prefix_go<T, 64>(tk, tv, p, s) : prefix_go<T, 128>(tk, tv, p, s);
 }
 
 }  // namespace
 }  // namespace fe
 
 extern "C" uint64_t fe_prefix_attention_workspace(const fe_prefix_args* a) {
-  return fe::check_prefix(a) == FE_OK ? 256 : 0;
+  using namespace fe;
+  if (check_prefix(a) != FE_OK) return 0;
+  const Device& dev = device();
+  if (dev.err != cudaSuccess) {
+    fail_cuda(dev.err, "fe_prefix_attention_workspace");
+    return 0;
+  }
+  return layout(a, dev.sms, most_tiles(a)).bytes;
 }
 
 extern "C" int fe_prefix_attention(const fe_prefix_args* a, void* stream) {
@@ -133,8 +1256,23 @@ extern "C" int fe_prefix_attention(const fe_prefix_args* a, void* stream) {
   if (rc != FE_OK) return rc;
   if (a->n_rows == 0) return FE_OK;
   if (!a->workspace || misaligned(a->workspace, 256)) return fail(FE_ERR_INVALID_ARG, "workspace null or not 256-byte aligned");
-  if (a->workspace_bytes < fe_prefix_attention_workspace(a)) return fail(FE_ERR_WORKSPACE, "workspace too small");
+  const Device& dev = device();
+  if (dev.err != cudaSuccess) return fail_cuda(dev.err, "fe_prefix_attention");
   PrefixParams p{};
+  p.ctas = dev.sms;
+  p.max_tiles = most_tiles(a);
+  const Layout w = layout(a, p.ctas, p.max_tiles);
+  if (a->workspace_bytes < w.bytes) return fail(FE_ERR_WORKSPACE, "workspace too small");
+  char* ws = static_cast<char*>(a->workspace);
+  p.head = reinterpret_cast<PlanHead*>(ws + w.head);
+  p.gtile = reinterpret_cast<int*>(ws + w.gtile);
+  p.gcost = reinterpret_cast<long long*>(ws + w.gcost);
+  p.cost = reinterpret_cast<int*>(ws + w.cost);
+  p.before = reinterpret_cast<long long*>(ws + w.before);
+  p.recs = reinterpret_cast<SplitRec*>(ws + w.recs);
+  p.list = reinterpret_cast<int*>(ws + w.list);
+  p.part_o = reinterpret_cast<float*>(ws + w.part_o);
+  p.part_ml = reinterpret_cast<float2*>(ws + w.part_ml);
   p.group_start = a->group_start;
   p.prefix_len = a->prefix_len;
   p.prefix_pages = a->prefix_pages;
@@ -154,13 +1292,18 @@ extern "C" int fe_prefix_attention(const fe_prefix_args* a, void* stream) {
   p.n_rows = a->n_rows;
   p.hq = a->q_heads;
   p.hkv = a->kv.kv_heads;
+  p.hr = p.hq / p.hkv;
   p.prefix_cols = a->prefix_cols;
   p.page_cols = a->page_cols;
   p.page_rows = a->kv.page_rows;
   p.n_pages = a->kv.n_pages;
   p.scale = a->scale;
+  p.sc = std::fmax((float)(a->scale * 1.4426950408889634), 1e-30f);
+  CUtensorMap tk, tv;
+  if (!encode_pages(&tk, a->kv, a->kv.k) || !encode_pages(&tv, a->kv, a->kv.v))
+    return fail(FE_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = a->kv.dtype == FE_IO_BF16 ? prefix_dim<__nv_bfloat16>(p, a->kv.head_dim, s)
-                                                  : prefix_dim<__half>(p, a->kv.head_dim, s);
+  const cudaError_t e = a->kv.dtype == FE_IO_BF16 ? prefix_dim<__nv_bfloat16>(tk, tv, p, a->kv.head_dim, s)
+                                                  : prefix_dim<__half>(tk, tv, p, a->kv.head_dim, s);
   return e == cudaSuccess ? FE_OK : fail_cuda(e, "fe_prefix_attention");
 }
