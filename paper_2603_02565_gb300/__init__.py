@@ -15,7 +15,8 @@ __all__ += _GENERATION
 def __getattr__(name):
     if name in _GENERATION:
         from . import generation
-        return getattr(generation, name)
+        value = globals()[name] = getattr(generation, name)  # found at once the next time
+        return value
     if name in __all__:
         from . import binding
         return getattr(binding, name)

@@ -50,40 +50,6 @@ class FeConfig(ctypes.Structure):
                 ("linear_context_attn", ctypes.c_int32)]
 
 
-class FePagedKv(ctypes.Structure):
-    _fields_ = [("dtype", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32),
-                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("k", ctypes.c_void_p),
-                ("v", ctypes.c_void_p)]
-
-
-class FeAppendArgs(ctypes.Structure):
-    _fields_ = ([("kv", FePagedKv)]
-                + [(n, ctypes.c_int32) for n in ("n_seqs", "n_rows", "page_cols", "q_heads", "rope_rows", "rot_dim",
-                                                 "pairs", "reserved")]
-                + [(n, ctypes.c_void_p) for n in ("row_start", "first", "shift", "pages", "k", "v", "q")]
-                + [(n, ctypes.c_int64) for n in ("k_row", "k_head", "v_row", "v_head", "q_row", "q_head")]
-                + [(n, ctypes.c_void_p) for n in ("q_out", "rope", "status")])
-
-
-class FePrefixArgs(ctypes.Structure):
-    _fields_ = ([("kv", FePagedKv)]
-                + [(n, ctypes.c_int32) for n in ("n_groups", "n_seqs", "n_rows", "q_heads", "prefix_cols", "page_cols")]
-                + [("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
-                + [(n, ctypes.c_void_p) for n in ("group_start", "prefix_len", "prefix_pages", "row_start", "seq_len",
-                                                  "pages", "q")]
-                + [(n, ctypes.c_int64) for n in ("q_row", "q_head")]
-                + [(n, ctypes.c_void_p) for n in ("out", "lse", "workspace")]
-                + [("workspace_bytes", ctypes.c_uint64), ("status", ctypes.c_void_p)])
-
-
-class FePolicyArgs(ctypes.Structure):
-    _fields_ = ([(n, ctypes.c_int32) for n in ("dtype", "rows", "vocab")]
-                + [(n, ctypes.c_float) for n in ("clip_low", "clip_high", "beta", "temperature", "grad_scale")]
-                + [("logits", ctypes.c_void_p), ("logits_row", ctypes.c_int64), ("grad_row", ctypes.c_int64)]
-                + [(n, ctypes.c_void_p) for n in ("tokens", "advantages", "weights", "old_logp", "ref_logp", "loss",
-                                                  "terms", "logp", "lse", "coef", "grad", "status")])
-
-
 class FeError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"fe error {code}: {msg}")
@@ -140,15 +106,15 @@ def load_library(path: str = LIB_PATH):
     L.fe_kernels_per_batch.restype = i32
     L.fe_distinct_layout_noalloc.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp]
     L.fe_distinct_layout_noalloc.restype = i32
-    L.fe_kv_append.argtypes = [ctypes.POINTER(FeAppendArgs), vp]
+    L.fe_kv_append.argtypes = [vp, vp]  # (a packed fe_append_args, stream)
     L.fe_kv_append.restype = i32
-    L.fe_prefix_attention_workspace.argtypes = [ctypes.POINTER(FePrefixArgs)]
+    L.fe_prefix_attention_workspace.argtypes = [vp]
     L.fe_prefix_attention_workspace.restype = ctypes.c_uint64
-    L.fe_prefix_attention.argtypes = [ctypes.POINTER(FePrefixArgs), vp]
+    L.fe_prefix_attention.argtypes = [vp, vp]
     L.fe_prefix_attention.restype = i32
-    L.fe_policy_loss.argtypes = [ctypes.POINTER(FePolicyArgs), vp]
+    L.fe_policy_loss.argtypes = [vp, vp]
     L.fe_policy_loss.restype = i32
-    L.fe_policy_loss_backward.argtypes = [ctypes.POINTER(FePolicyArgs), vp, vp]
+    L.fe_policy_loss_backward.argtypes = [vp, vp, vp]
     L.fe_policy_loss_backward.restype = i32
     L.fe_destroy.argtypes = [vp]
     L.fe_destroy.restype = i32

@@ -17,9 +17,8 @@ CUDA int32 tensor of one element that the caller zeroes and `check_status` reads
 """
 from __future__ import annotations
 
-import collections
-import ctypes
 import math
+import struct
 
 import torch
 
@@ -28,6 +27,19 @@ from .binding import FeError, _check, load_library
 
 _TYPES = {torch.bfloat16: _b.FE_IO_BF16, torch.float16: _b.FE_IO_F16, torch.float32: _b.FE_IO_F32}
 _PAIRS = {"half": 0, "interleaved": 1}
+# The argument structures of fe.h, fields in their order.  (A call of a few microseconds on the GPU is worth a lean
+# one here: packing all fields at once takes a tenth of the time that setting them one by one does.)
+_APPEND = struct.Struct("@5i2P8i7P6q3P")
+_PREFIX = struct.Struct("@5i2P6ifi7P2q3PQP")
+_POLICY = struct.Struct("@3i5fP2q12P")
+_LIB = None
+
+
+def _lib():
+    global _LIB
+    if _LIB is None:
+        _LIB = load_library()
+    return _LIB
 
 
 def check_status(status) -> None:
@@ -48,37 +60,60 @@ def rotary_table(n_positions: int, rot_dim: int, base: float = 10000.0, device="
     return torch.stack([a.cos(), a.sin()], -1).to(torch.float32).to(device)
 
 
-def _on(stream, device):
-    """(handle, torch stream to allocate for or None) of a `stream` argument."""
+# the current stream's handle by device index, without a stream object where torch offers that
+_current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def _stream_of(stream, index):
+    """(handle, torch stream to allocate for; None: the current one) of a `stream` argument."""
     if stream is None:
-        return torch.cuda.current_stream(device).cuda_stream, None
+        return _current(index), None
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream), device=device)
+        stream = torch.cuda.ExternalStream(int(stream), device=index)
     return stream.cuda_stream, stream
 
 
-def _empty(on, make):
+def _like(t, on):
+    """A contiguous tensor of t's shape and type, allocated for stream `on`."""
     if on is None:
-        return make()
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
     with torch.cuda.stream(on):
-        return make()
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
-def _i32(name, t, shape, device):
-    """The pointer of a contiguous int32 CUDA tensor; None in `shape` stands for any size."""
-    if t.dtype != torch.int32 or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor on {device}")
-    if t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
-        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+def _new(t, shape, on, dtype=None):
+    if on is None:
+        return torch.empty(shape, dtype=dtype or t.dtype, device=t.device)
+    with torch.cuda.stream(on):
+        return torch.empty(shape, dtype=dtype or t.dtype, device=t.device)
+
+
+def _i32(name, t, n, index):
+    """The pointer of a contiguous int32 tensor [n] on CUDA device `index`."""
+    if t.dtype is not torch.int32 or t.shape != (n,) or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor [{n}] on cuda:{index}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _f32(name, t, n, device):
+def _table(name, t, n, index):
+    """(pointer, columns) of a contiguous int32 table [n, columns]."""
+    if t.dtype is not torch.int32 or t.dim() != 2 or t.get_device() != index or not t.is_contiguous() or t.shape[0] != n:
+        raise ValueError(f"{name} must be a contiguous int32 tensor [{n}, columns] on cuda:{index}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    return t.data_ptr(), t.shape[1]
+
+
+def _f32(name, t, n, index):
     if t is None:
-        return None
-    if t.dtype != torch.float32 or t.device != device or not t.is_contiguous() or t.numel() != n:
-        raise ValueError(f"{name} must be a contiguous float32 tensor of {n} elements on {device}")
+        return 0
+    if t.dtype is not torch.float32 or t.get_device() != index or not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"{name} must be a contiguous float32 tensor of {n} elements on cuda:{index}")
     return t.data_ptr()
+
+
+def _status(status, index):
+    return 0 if status is None else _i32("status", status, 1, index)
 
 
 class PagedKV:
@@ -87,26 +122,37 @@ class PagedKV:
     c % page_rows of the page that entry c // page_rows of its page-table row names."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
-        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in _TYPES or k.device != v.device:
-            raise ValueError("k and v must be [n_pages, kv_heads, page_rows, head_dim] of one type on one device")
-        if not (k.is_cuda and k.is_contiguous() and v.is_contiguous()):
-            raise ValueError("k and v must be contiguous CUDA tensors")
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("k and v must be [n_pages, kv_heads, page_rows, head_dim], both bf16 or both f16")
+        if not (k.is_cuda and k.device == v.device and k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("k and v must be contiguous CUDA tensors on one device")
         self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
         self.n_pages, self.kv_heads, self.page_rows, self.head_dim = k.shape
-        self._kv = _b.FePagedKv(_TYPES[k.dtype], *k.shape[:1], k.shape[2], k.shape[1], k.shape[3], k.data_ptr(),
-                                v.data_ptr())
+        self._index = k.get_device()
+        self._fields = (_TYPES[k.dtype], self.n_pages, self.page_rows, self.kv_heads, self.head_dim, k.data_ptr(),
+                        v.data_ptr())
+        self._scale = 1.0 / math.sqrt(self.head_dim)
+        self._workspace = {}  # bytes by sizes
 
     @classmethod
     def empty(cls, n_pages, page_rows, kv_heads, head_dim, dtype=torch.bfloat16, device="cuda"):
         shape = (n_pages, kv_heads, page_rows, head_dim)
         return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device))
 
-    def _rows(self, name, x, heads=None):
-        if x.dim() != 3 or x.dtype != self.dtype or x.device != self.device or x.shape[2] != self.head_dim or (
-                heads is not None and x.shape[1] != heads) or (x.stride(2) != 1 and x.numel() > 0):
-            raise ValueError(f"{name} must be [rows, {heads or 'heads'}, {self.head_dim}] of {self.dtype} on "
-                             f"{self.device}, its last dimension contiguous")
-        return x.data_ptr()
+    def _rows(self, name, x, n, heads=None):
+        """(pointer, heads, row stride, head stride) of rows [n, heads, head_dim]."""
+        if x.dim() == 3 and x.dtype is self.dtype and x.get_device() == self._index:
+            rows, h, d = x.shape
+            row, head, one = x.stride()
+            if rows == n and d == self.head_dim and (one == 1 or rows == 0) and (heads is None or h == heads):
+                return x.data_ptr(), h, row, head
+        raise ValueError(f"{name} must be [{n}, {heads or 'heads'}, {self.head_dim}] of {self.dtype} on {self.device}, "
+                         f"its last dimension contiguous; got {x.dtype} {tuple(x.shape)} on {x.device}")
+
+    def _out(self, name, x, like):
+        if x.shape != like.shape or x.dtype is not like.dtype or x.get_device() != self._index or not x.is_contiguous():
+            raise ValueError(f"{name} must be contiguous, with q's shape, type and device")
+        return x
 
     def append(self, k, v, row_start, first, pages, *, q=None, rope=None, pairs="half", shift=None, q_out=None,
                status=None, stream=None):
@@ -117,42 +163,32 @@ class PagedKV:
         pages[s].  With rope ([positions, rot_dim / 2, 2] fp32, see rotary_table) keys, and the queries
         q [rows, q_heads, head_dim] when given, are rotated at position shift[s] + first[s] + j; pairs: "half"
         or "interleaved".  Returns the rotated queries (q_out, contiguous), or None without q."""
-        dev = self.device
-        a = _b.FeAppendArgs(kv=self._kv)
-        a.n_seqs, a.n_rows = first.shape[0], k.shape[0]
-        a.k, a.v = self._rows("k", k, self.kv_heads), self._rows("v", v, self.kv_heads)
-        if v.shape[0] != a.n_rows:
-            raise ValueError("k and v must have as many rows")
-        a.k_row, a.k_head, _ = k.stride()
-        a.v_row, a.v_head, _ = v.stride()
-        a.row_start = _i32("row_start", row_start, (a.n_seqs + 1,), dev)
-        a.first = _i32("first", first, (a.n_seqs,), dev)
-        a.pages = _i32("pages", pages, (a.n_seqs, None), dev)
-        a.page_cols = pages.shape[1]
-        if shift is not None:
-            a.shift = _i32("shift", shift, (a.n_seqs,), dev)
+        dev = self._index
+        S, T = first.shape[0], k.shape[0]
+        kp, _, k_row, k_head = self._rows("k", k, T, self.kv_heads)
+        vp, _, v_row, v_head = self._rows("v", v, T, self.kv_heads)
         if pairs not in _PAIRS:
             raise ValueError("pairs must be 'half' or 'interleaved'")
-        a.pairs = _PAIRS[pairs]
+        rope_p = rope_rows = rot = 0
         if rope is not None:
             if rope.dim() != 3 or rope.shape[2] != 2:
                 raise ValueError("rope must be [positions, rot_dim / 2, 2]")
-            a.rope = _f32("rope", rope, rope.numel(), dev)
-            a.rope_rows, a.rot_dim = rope.shape[0], 2 * rope.shape[1]
-        if status is not None:
-            a.status = _i32("status", status, (1,), dev)
-        handle, on = _on(stream, dev)
+            rope_rows, half, _ = rope.shape
+            rot = 2 * half
+            rope_p = _f32("rope", rope, rope_rows * rot, dev)
+        table, cols = _table("pages", pages, S, dev)
+        handle, on = _stream_of(stream, dev)
+        qp = hq = q_row = q_head = out_p = 0
         if q is not None:
-            a.q, a.q_heads = self._rows("q", q), q.shape[1]
-            if q.shape[0] != a.n_rows:
-                raise ValueError("q and k must have as many rows")
-            a.q_row, a.q_head, _ = q.stride()
-            if q_out is None:
-                q_out = _empty(on, lambda: torch.empty(q.shape, dtype=q.dtype, device=dev))
-            elif q_out.shape != q.shape or not q_out.is_contiguous():
-                raise ValueError("q_out must be contiguous and have q's shape")
-            a.q_out = self._rows("q_out", q_out)
-        _check(load_library().fe_kv_append(ctypes.byref(a), handle))
+            qp, hq, q_row, q_head = self._rows("q", q, T)
+            q_out = _like(q, on) if q_out is None else self._out("q_out", q_out, q)
+            out_p = q_out.data_ptr()
+        rc = _lib().fe_kv_append(_APPEND.pack(
+            *self._fields, S, T, cols, hq, rope_rows, rot, _PAIRS[pairs], 0, _i32("row_start", row_start, S + 1, dev),
+            _i32("first", first, S, dev), 0 if shift is None else _i32("shift", shift, S, dev), table, kp, vp, qp, k_row,
+            k_head, v_row, v_head, q_row, q_head, out_p, rope_p, _status(status, dev)), handle)
+        if rc:
+            _check(rc)
         return q_out if q is not None else None
 
     def attend(self, q, row_start, lengths, pages, group_start, prefix_lengths, prefix_pages, *, scale=None, out=None,
@@ -165,117 +201,128 @@ class PagedKV:
         unless given.  Returns out [rows, q_heads, head_dim], with with_lse (out, lse [rows, q_heads] fp32); a
         row that sees nothing gets 0 and -inf.  workspace: a uint8 tensor to use instead of a fresh one
         (workspace_bytes says how much); not to be shared by calls that may overlap."""
-        dev = self.device
-        a = _b.FePrefixArgs(kv=self._kv)
-        a.n_groups, a.n_seqs, a.n_rows = prefix_lengths.shape[0], lengths.shape[0], q.shape[0]
-        a.q, a.q_heads = self._rows("q", q), q.shape[1]
-        a.q_row, a.q_head, _ = q.stride()
-        a.row_start = _i32("row_start", row_start, (a.n_seqs + 1,), dev)
-        a.seq_len = _i32("lengths", lengths, (a.n_seqs,), dev)
-        a.pages = _i32("pages", pages, (a.n_seqs, None), dev)
-        a.page_cols = pages.shape[1]
-        a.group_start = _i32("group_start", group_start, (a.n_groups + 1,), dev)
-        a.prefix_len = _i32("prefix_lengths", prefix_lengths, (a.n_groups,), dev)
-        a.prefix_pages = _i32("prefix_pages", prefix_pages, (a.n_groups, None), dev)
-        a.prefix_cols = prefix_pages.shape[1]
-        a.scale = 1.0 / math.sqrt(self.head_dim) if scale is None else scale
-        if status is not None:
-            a.status = _i32("status", status, (1,), dev)
-        handle, on = _on(stream, dev)
-        if out is None:
-            out = _empty(on, lambda: torch.empty(q.shape, dtype=q.dtype, device=dev))
-        elif out.shape != q.shape or not out.is_contiguous():
-            raise ValueError("out must be contiguous and have q's shape")
-        a.out = self._rows("out", out)
-        lse = None
-        if with_lse:
-            lse = _empty(on, lambda: torch.empty(q.shape[:2], dtype=torch.float32, device=dev))
-            a.lse = lse.data_ptr()
-        lib = load_library()
+        dev = self._index
+        G, S, T = prefix_lengths.shape[0], lengths.shape[0], q.shape[0]
+        qp, hq, q_row, q_head = self._rows("q", q, T)
+        table, cols = _table("pages", pages, S, dev)
+        pre_table, pre_cols = _table("prefix_pages", prefix_pages, G, dev)
+        handle, on = _stream_of(stream, dev)
+        out = _like(q, on) if out is None else self._out("out", out, q)
+        lse = _new(q, (T, hq), on, torch.float32) if with_lse else None
         if workspace is None:
-            n = lib.fe_prefix_attention_workspace(ctypes.byref(a))
-            workspace = _empty(on, lambda: torch.empty(n, dtype=torch.uint8, device=dev))
-        elif workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
-            raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
-        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-        _check(lib.fe_prefix_attention(ctypes.byref(a), handle))
+            need = self._workspace.get((G, S, T, hq))
+            if need is None:
+                need = self._workspace[G, S, T, hq] = self.workspace_bytes(G, S, T, hq)
+            workspace = _new(q, (need + 1) // 2, on)
+        elif workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous uint8 tensor on {self.device}")
+        else:
+            need = workspace.numel()
+        rc = _lib().fe_prefix_attention(_PREFIX.pack(
+            *self._fields, G, S, T, hq, pre_cols, cols, self._scale if scale is None else scale, 0,
+            _i32("group_start", group_start, G + 1, dev), _i32("prefix_lengths", prefix_lengths, G, dev), pre_table,
+            _i32("row_start", row_start, S + 1, dev), _i32("lengths", lengths, S, dev), table, qp, q_row, q_head,
+            out.data_ptr(), 0 if lse is None else lse.data_ptr(), workspace.data_ptr(), need, _status(status, dev)), handle)
+        if rc:
+            _check(rc)
         return (out, lse) if with_lse else out
 
     def workspace_bytes(self, n_groups: int, n_seqs: int, n_rows: int, q_heads: int) -> int:
         """Workspace of attend for these sizes."""
-        one = self.k.data_ptr()  # (any pointer: only sizes count)
-        a = _b.FePrefixArgs(kv=self._kv, n_groups=n_groups, n_seqs=n_seqs, n_rows=n_rows, q_heads=q_heads, prefix_cols=1,
-                            page_cols=1, scale=1.0, group_start=one, prefix_len=one, prefix_pages=one, row_start=one,
-                            seq_len=one, pages=one, q=one, out=one, q_row=8, q_head=8)
-        n = load_library().fe_prefix_attention_workspace(ctypes.byref(a))
+        at = self._fields[5]  # (any pointer: only sizes count)
+        n = _lib().fe_prefix_attention_workspace(_PREFIX.pack(
+            *self._fields, n_groups, n_seqs, n_rows, q_heads, 1, 1, 1.0, 0, at, at, at, at, at, at, at, 8, 8, at, 0, 0, 0, 0))
         if n == 0:
-            raise FeError(_b.FE_ERR_INVALID_ARG, load_library().fe_last_error_message().decode())
+            raise FeError(_b.FE_ERR_INVALID_ARG, _lib().fe_last_error_message().decode())
         return int(n)
 
 
-PolicyLoss = collections.namedtuple("PolicyLoss", "loss terms logp lse coef grad")
-PolicyLoss.__doc__ = """Outputs of policy_loss: loss (a 0-d tensor), and per token the weighted term, log probability,
-logsumexp and the slope of the loss to the log probability; grad [tokens, vocab] or None."""
+class PolicyLoss:
+    """Outputs of policy_loss: loss (a 0-d tensor), and per token terms (the weighted summands), logp (log
+    probability), lse (logsumexp) and coef (the slope of the loss to logp), all fp32; grad [tokens, vocab] or None."""
+
+    __slots__ = ("_stats", "grad")
+
+    def __init__(self, stats, grad):
+        self._stats, self.grad = stats, grad  # [1 + 4 tokens]: the loss, then the four rows
+
+    def _row(self, i):
+        n = (self._stats.shape[0] - 1) // 4
+        return self._stats[1 + i * n:1 + (i + 1) * n]
+
+    loss = property(lambda self: self._stats[0])
+    terms = property(lambda self: self._row(0))
+    logp = property(lambda self: self._row(1))
+    lse = property(lambda self: self._row(2))
+    coef = property(lambda self: self._row(3))
 
 
-def _policy_args(logits, tokens, weights, temperature, grad_scale, status):
-    if logits.dim() != 2 or logits.dtype not in _TYPES or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] > 1):
-        raise ValueError("logits must be a CUDA tensor [tokens, vocab] of bf16, f16 or fp32 with contiguous rows")
+def _logits(logits):
+    """(tokens, vocab, type, device index, row stride) of logits."""
+    if logits.dim() == 2 and logits.is_cuda and logits.dtype in _TYPES:
+        T, V = logits.shape
+        row, one = logits.stride()
+        if one == 1 or V <= 1:
+            return T, V, _TYPES[logits.dtype], logits.get_device(), row if T > 1 else max(V, row)
+    raise ValueError("logits must be a CUDA tensor [tokens, vocab] of bf16, f16 or fp32 with contiguous rows")
+
+
+def _grad(logits, row, grad, on):
+    """(tensor, row stride) of the gradient: a new one has its rows as far apart as the logits', the same alignment."""
+    if grad is None:
+        if logits.is_contiguous():
+            return _like(logits, on), row
+        if on is None:
+            return torch.empty_strided(logits.shape, (row, 1), dtype=logits.dtype, device=logits.device), row
+        with torch.cuda.stream(on):
+            return torch.empty_strided(logits.shape, (row, 1), dtype=logits.dtype, device=logits.device), row
     T, V = logits.shape
-    dev = logits.device
-    a = _b.FePolicyArgs(dtype=_TYPES[logits.dtype], rows=T, vocab=V, temperature=temperature, grad_scale=grad_scale)
-    a.logits, a.logits_row = logits.data_ptr(), logits.stride(0) if T > 1 else max(V, logits.stride(0))
-    a.tokens = _i32("tokens", tokens, (T,), dev)
-    a.weights = _f32("weights", weights, T, dev)
-    if status is not None:
-        a.status = _i32("status", status, (1,), dev)
-    return a
-
-
-def _policy_grad(a, logits, grad, on):
-    if grad is None:  # rows as far apart as the logits': the same alignment
-        grad = _empty(on, lambda: torch.empty_strided(logits.shape, (a.logits_row, 1), dtype=logits.dtype,
-                                                      device=logits.device))
-    elif grad.shape != logits.shape or grad.dtype != logits.dtype or grad.device != logits.device or (
-            grad.stride(1) != 1 and grad.shape[1] > 1):
+    if grad.shape != logits.shape or grad.dtype is not logits.dtype or grad.get_device() != logits.get_device() or (
+            grad.stride(1) != 1 and V > 1):
         raise ValueError("grad must have the logits' shape, type and device, and contiguous rows")
-    a.grad, a.grad_row = grad.data_ptr(), grad.stride(0) if a.rows > 1 else max(a.vocab, grad.stride(0))
-    return grad
+    return grad, grad.stride(0) if T > 1 else max(V, grad.stride(0))
 
 
 def policy_loss(logits, tokens, advantages, weights=None, *, old_logp=None, ref_logp=None, clip=(0.2, 0.2), beta=0.0,
                 temperature=1.0, with_grad=True, grad_scale=1.0, grad=None, status=None, stream=None) -> PolicyLoss:
     """Clipped policy loss with a KL term (fe_policy_loss), and its gradient to the logits.
 
-    logits [tokens, vocab] bf16, f16 or fp32; tokens int32, -- the chosen ones; advantages, weights (1 / tokens each
+    logits [tokens, vocab] bf16, f16 or fp32; tokens int32, the chosen ones; advantages, weights (1 / tokens each
     unless given; 0: the token takes no part), old_logp (None: the present policy's), ref_logp (None: no KL term)
     fp32.  clip: how far the ratio may go below and above 1; beta: the KL term's weight.  grad: where to
     write the gradient times grad_scale (may be logits itself)."""
-    a = _policy_args(logits, tokens, weights, temperature, grad_scale, status)
-    T, dev = a.rows, logits.device
-    a.advantages = _f32("advantages", advantages, T, dev)
-    a.old_logp = _f32("old_logp", old_logp, T, dev)
-    a.ref_logp = _f32("ref_logp", ref_logp, T, dev)
-    a.clip_low, a.clip_high = clip
-    a.beta = beta
-    handle, on = _on(stream, dev)
-    grad = _policy_grad(a, logits, grad, on) if with_grad else None
-    buf = _empty(on, lambda: torch.empty(4 * T + 1, dtype=torch.float32, device=dev))
-    at = buf.data_ptr()
-    a.loss, a.terms, a.logp, a.lse, a.coef = at, at + 4, at + 4 + 4 * T, at + 4 + 8 * T, at + 4 + 12 * T
-    _check(load_library().fe_policy_loss(ctypes.byref(a), handle))
-    return PolicyLoss(buf[0], *buf[1:].view(4, T).unbind(0), grad)
+    T, V, dtype, dev, row = _logits(logits)
+    handle, on = _stream_of(stream, dev)
+    grad_p = grad_row = 0
+    if with_grad:
+        grad, grad_row = _grad(logits, row, grad, on)
+        grad_p = grad.data_ptr()
+    else:
+        grad = None
+    stats = _new(logits, 4 * T + 1, on, torch.float32)
+    at, n = stats.data_ptr(), 4 * T
+    rc = _lib().fe_policy_loss(_POLICY.pack(
+        dtype, T, V, clip[0], clip[1], beta, temperature, grad_scale, logits.data_ptr(), row, grad_row,
+        _i32("tokens", tokens, T, dev), _f32("advantages", advantages, T, dev), _f32("weights", weights, T, dev),
+        _f32("old_logp", old_logp, T, dev), _f32("ref_logp", ref_logp, T, dev), at, at + 4, at + 4 + n, at + 4 + 2 * n,
+        at + 4 + 3 * n, grad_p, _status(status, dev)), handle)
+    if rc:
+        _check(rc)
+    return PolicyLoss(stats, grad)
 
 
 def policy_loss_backward(logits, tokens, result: PolicyLoss, weights=None, *, upstream=None, temperature=1.0,
                          grad_scale=1.0, grad=None, status=None, stream=None):
     """The gradient to the logits from an earlier policy_loss (with_grad=False) on the same tokens, weights and
     temperature, times upstream (a CUDA fp32 tensor of one element; None: 1) and grad_scale."""
-    a = _policy_args(logits, tokens, weights, temperature, grad_scale, status)
-    dev = logits.device
-    a.lse, a.coef = _f32("lse", result.lse, a.rows, dev), _f32("coef", result.coef, a.rows, dev)
-    up = _f32("upstream", upstream, 1, dev)
-    handle, on = _on(stream, dev)
-    grad = _policy_grad(a, logits, grad, on)
-    _check(load_library().fe_policy_loss_backward(ctypes.byref(a), up, handle))
+    T, V, dtype, dev, row = _logits(logits)
+    handle, on = _stream_of(stream, dev)
+    grad, grad_row = _grad(logits, row, grad, on)
+    rc = _lib().fe_policy_loss_backward(_POLICY.pack(
+        dtype, T, V, 0.0, 0.0, 0.0, temperature, grad_scale, logits.data_ptr(), row, grad_row,
+        _i32("tokens", tokens, T, dev), 0, _f32("weights", weights, T, dev), 0, 0, 0, 0, 0,
+        _f32("lse", result.lse, T, dev), _f32("coef", result.coef, T, dev), grad.data_ptr(), _status(status, dev)),
+        _f32("upstream", upstream, 1, dev), handle)
+    if rc:
+        _check(rc)
     return grad
