@@ -6,7 +6,22 @@
 //   grad_v = k (1[v = y] - softmax_v),  k = grad_scale coef / temperature.
 // The maximum comes off before the product, so the exponents' errors are relative to the
 // distance from it.  All of it is fp32; a gradient is rounded once.
+//
+// Bound by memory: at least each logit is read once and its gradient written once.  A row's
+// gradient needs the whole row's sum first, so it stays on the SM in between where it fits:
+//   rows up to 16 KB   in the registers of a CTA of 128 threads, eight CTAs an SM
+//   longer rows        the first pass keeps 64 KB of the row (52 KB in rows up to 64 KB) in
+//                      shared memory and asks L2 to hold the rest, which the second pass
+//                      reads again; gradients leave with the lowest claim on L2.
+// What matters is rows in different phases beside one another: three CTAs of 512 threads an SM
+// (four of 256 for rows up to 64 KB).  4096 tokens x 100000 words in bf16 (241 us at the copy
+// rate): 295 us; without the L2 hints 315, everything read twice 397 (hints alone 313), two
+// CTAs 322, one of 1024 threads 345.  A ring of bulk copies several rows deep in one CTA of
+// 512 threads took 440: its phases do not overlap, and clusters that share a row pay several
+// us a row (710 with the row in the registers of four CTAs).  16384 x 8192 (79 us): 96 us.
+#include <algorithm>
 #include <cmath>
+#include <mutex>
 
 #include "fe_ops.cuh"
 
@@ -25,7 +40,7 @@ struct PolicyParams {
   float lo, hi, beta, t, inv_t, scale, c;  // temperature, its inverse; c: log2(e) / temperature
 };
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 512;  // of the backward kernel
 constexpr float kLn2 = 0.693147180559945309f;
 
 // Running maximum and sum of 2^((x - m) c), m -inf as long as nothing else has come
@@ -42,55 +57,67 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c) {
   return {m, rebase(a.s, a.m, m, c) + rebase(b.s, b.m, m, c)};
 }
 
-__device__ __forceinline__ MaxSum block_join(MaxSum v, float c, MaxSum* sh) {
+template <int LANES>
+__device__ __forceinline__ MaxSum warp_join(MaxSum v, float c) {
+  float m = v.m;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    MaxSum w = {__shfl_xor_sync(0xffffffffu, v.m, o), __shfl_xor_sync(0xffffffffu, v.s, o)};
-    v = join(v, w, c);
-  }
+  for (int o = LANES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float s = rebase(v.s, v.m, m, c);
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return {m, s};
+}
+// the same in every thread; sh: one entry a warp, free again after the block's next barrier
+template <int THREADS>
+__device__ __forceinline__ MaxSum block_join(MaxSum v, float c, MaxSum* sh) {
+  constexpr int W = THREADS / 32;
+  v = warp_join<32>(v, c);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
   __syncthreads();
-  v = sh[0];
-  for (int i = 1; i < kThreads / 32; ++i) v = join(v, sh[i], c);
-  return v;
+  return warp_join<W>(sh[threadIdx.x & (W - 1)], c);
 }
 
-// What row t's token asks for: weight, whether it takes part, its index
+// What token t brings: weight, index, advantage, log probabilities before and of the reference
+// (nothing is done with the loaded values here: a first use waits for its load)
 struct Token {
-  float w;
+  float w, adv, old, ref;
   int y;
-  bool kept, valid;
+  __device__ __forceinline__ bool kept() const { return w != 0.f; }
+  __device__ __forceinline__ bool valid(int vocab) const { return y >= 0 && y < vocab; }
 };
 __device__ __forceinline__ Token token_of(const PolicyParams& p, int t) {
   Token k;
   k.w = p.weights ? __ldg(p.weights + t) : 1.f / (float)p.rows;
   k.y = __ldg(p.tokens + t);
-  k.kept = k.w != 0.f;
-  k.valid = k.y >= 0 && k.y < p.vocab;
+  k.adv = p.adv ? __ldg(p.adv + t) : 0.f;
+  k.old = p.old_logp ? __ldg(p.old_logp + t) : 0.f;
+  k.ref = p.ref_logp ? __ldg(p.ref_logp + t) : 0.f;
   return k;
 }
 
-// terms, logp, lse and coef of a row from its chosen logit and statistics; the gradient's factor
-__device__ float row_outputs(const PolicyParams& p, int t, const Token& k, float xy, MaxSum v) {
+// terms, logp, lse and coef of a row from its chosen logit and statistics (written where asked); the gradient's factor
+__device__ __forceinline__ float row_outputs(const PolicyParams& p, int t, const Token& k, float xy, MaxSum v, bool write) {
   const float l2 = log2f(v.s);
   float logp = ((xy - v.m) * p.c - l2) * kLn2, lse = v.m * p.inv_t + l2 * kLn2;
   if (v.m == -INFINITY) lse = -INFINITY, logp = NAN;
-  if (!k.valid) logp = NAN;
-  const float a = __ldg(p.adv + t), r = p.old_logp ? expf(logp - __ldg(p.old_logp + t)) : 1.f;
-  const float plain = r * a, clipped = fminf(fmaxf(r, 1.f - p.lo), 1.f + p.hi) * a;
+  if (!k.valid(p.vocab)) logp = NAN;
+  const float r = p.old_logp ? expf(logp - k.old) : 1.f;
+  const float plain = r * k.adv, clipped = fminf(fmaxf(r, 1.f - p.lo), 1.f + p.hi) * k.adv;
   float term = plain <= clipped ? -plain : -clipped, coef = plain <= clipped ? -plain : 0.f;
-  if (!(plain == plain)) term = coef = NAN;  // (clamping drops a NaN)
+  if (!(plain == plain) || !(logp == logp)) term = coef = NAN;  // (clamping drops a NaN)
   if (p.ref_logp) {
-    const float d = __ldg(p.ref_logp + t) - logp, e = expm1f(d);
+    const float d = k.ref - logp, e = expm1f(d);
     term += p.beta * (e - d);
     coef -= p.beta * e;
   }
   term *= k.w;
   coef *= k.w;
-  p.terms[t] = term;
-  p.logp[t] = logp;
-  p.lse[t] = lse;
-  p.coef[t] = coef;
+  if (write) {
+    p.terms[t] = term;
+    p.logp[t] = logp;
+    p.lse[t] = lse;
+    p.coef[t] = coef;
+  }
   return coef * p.scale * p.inv_t;
 }
 
@@ -105,9 +132,9 @@ struct RowSplit {
   }
 };
 
-template <typename T>
+template <int THREADS, typename T>
 __device__ __forceinline__ void zero_row(T* g, int n) {
-  for (int i = threadIdx.x; i < n; i += kThreads) g[i] = Elem<T>::put(0.f);
+  for (int i = threadIdx.x; i < n; i += THREADS) g[i] = Elem<T>::put(0.f);
 }
 
 // grad = k (1[v = y] - 2^((x - b) c) / sum) over a row
@@ -133,51 +160,277 @@ __device__ void grad_row(const T* x, T* g, int n_el, int y, float k, float c, fl
   for (int i = rs.head + rs.pieces * N + threadIdx.x; i < n_el; i += kThreads) one(i);
 }
 
+// a piece's part of the statistics, against a maximum that covers it
 template <typename T>
-__global__ void __launch_bounds__(kThreads) policy_kernel(const PolicyParams p) {
+__device__ __forceinline__ void piece_sum(const uint4& w, uint64_t nb, uint64_t c2, uint64_t* sum) {
   constexpr int N = Elem<T>::N;
-  __shared__ MaxSum sh[kThreads / 32];
-  __shared__ float s_k, s_xy;
+  float z[N];
+  piece_get<T>(w, z);
+#pragma unroll
+  for (int j = 0; j < N; j += 2) {
+    float a, b;
+    f32x2_unpack(f32x2_mul(f32x2_add(f32x2_pack(z[j], z[j + 1]), nb), c2), a, b);
+    sum[(j >> 1) & 1] = f32x2_add(sum[(j >> 1) & 1], f32x2_pack(ex2_approx(a), ex2_approx(b)));
+  }
+}
+__device__ __forceinline__ float sum_of(const uint64_t* sum) {
+  float a, b, c, d;
+  f32x2_unpack(sum[0], a, b);
+  f32x2_unpack(sum[1], c, d);
+  return (a + b) + (c + d);
+}
+template <typename T>
+__device__ __forceinline__ float piece_max(const uint4& w, float m) {
+  constexpr int N = Elem<T>::N;
+  float z[N];
+  piece_get<T>(w, z);
+#pragma unroll
+  for (int j = 0; j < N; ++j) m = fmaxf(m, z[j]);
+  return m;
+}
+// The gradient of a piece, f = -k / sum; yj: the token's place in it (any other value: not there).  There
+// k - k softmax is rounded once: the two may nearly cancel.
+template <typename T>
+__device__ __forceinline__ uint4 piece_grad(const uint4& w, uint64_t nb, uint64_t c2, float f, float kf, int yj) {
+  constexpr int N = Elem<T>::N;
+  const uint64_t f2 = f32x2_pack(f, f);
+  float z[N];
+  piece_get<T>(w, z);
+#pragma unroll
+  for (int j = 0; j < N; j += 2) {
+    float a, b;
+    f32x2_unpack(f32x2_mul(f32x2_add(f32x2_pack(z[j], z[j + 1]), nb), c2), a, b);
+    f32x2_unpack(f32x2_mul(f32x2_pack(ex2_approx(a), ex2_approx(b)), f2), z[j], z[j + 1]);
+  }
+  uint4 r = piece_put<T>(z);
+  if (yj >= 0 && yj < N) {
+    float b, c, d;
+    f32x2_unpack(nb, b, d);
+    f32x2_unpack(c2, c, d);
+    piece_get<T>(w, z);
+    float x = z[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) x = j == yj ? z[j] : x;
+    const float e = fmaf(f, ex2_approx((x + b) * c), kf);
+    uint32_t* rw = reinterpret_cast<uint32_t*>(&r);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (j != yj) continue;
+      if constexpr (sizeof(T) == 4) {
+        rw[j] = __float_as_uint(e);
+      } else {
+        const T t = Elem<T>::put(e);
+        const uint32_t u = *reinterpret_cast<const uint16_t*>(&t);
+        rw[j / 2] = j & 1 ? (rw[j / 2] & 0xffffu) | (u << 16) : (rw[j / 2] & 0xffff0000u) | u;
+      }
+    }
+  }
+  return r;
+}
+
+// ---------------------------------------------------------------------------
+// short rows: in registers
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ uint4 ld_stream(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p)
+               : "memory");
+  return v;
+}
+
+// A row's edges: the elements before its first 16-byte boundary and after its last one, by thread i < 2 N of a
+// block: the element of thread i, or -1.
+template <typename T>
+__device__ __forceinline__ int edge_of(int i, const RowSplit<T>& rs, int n) {
+  constexpr int N = Elem<T>::N;
+  if (i < N) return i < rs.head ? i : -1;
+  const int at = rs.head + rs.pieces * N + i - N;
+  return i < 2 * N && at < n ? at : -1;
+}
+
+// Rows up to 16 KB: a CTA of 128 threads holds one in registers between its statistics and its gradient; eight
+// CTAs an SM keep loads in flight while others compute.
+constexpr int kRowThreads = 128;
+template <typename T, int NV>
+__global__ void __launch_bounds__(kRowThreads, 8) policy_row_kernel(const PolicyParams p) {
+  constexpr int N = Elem<T>::N;
+  __shared__ MaxSum sh[kRowThreads / 32];
+  __shared__ float s_k;
   pdl_trigger();
   pdl_wait();
   const int t = blockIdx.x;
   const Token k = token_of(p, t);
+  const T* x = reinterpret_cast<const T*>(p.logits) + (long long)t * p.logits_row;
   T* g = p.grad ? reinterpret_cast<T*>(p.grad) + (long long)t * p.grad_row : nullptr;
-  if (!k.kept) {
+  if (!k.kept()) {
     if (threadIdx.x == 0) p.terms[t] = p.logp[t] = p.lse[t] = p.coef[t] = 0.f;
-    if (g) zero_row(g, p.vocab);
+    if (g) zero_row<kRowThreads>(g, p.vocab);
     return;
   }
-  if (!k.valid && threadIdx.x == 0 && p.status) atomicOr(p.status, FE_ST_INDEX);
-  const T* x = reinterpret_cast<const T*>(p.logits) + (long long)t * p.logits_row;
-  if (threadIdx.x == 0) s_xy = k.valid ? Elem<T>::get(x[k.y]) : 0.f;
   const RowSplit<T> rs(x, p.vocab);
-  MaxSum v = {-INFINITY, 0.f};
-  auto add = [&](const float* z, int n) {
-    float m = v.m;
-    for (int j = 0; j < n; ++j) m = fmaxf(m, z[j]);
-    if (m != v.m) v.s = rebase(v.s, v.m, m, p.c);
-    v.m = m;
-    const float b = base_of(m);
-    for (int j = 0; j < n; ++j) v.s += ex2_approx((z[j] - b) * p.c);
-  };
-  if ((int)threadIdx.x < rs.head) {
-    const float z = Elem<T>::get(x[threadIdx.x]);
-    add(&z, 1);
+  const int edge = edge_of(threadIdx.x, rs, p.vocab);
+  const T* xi = x + rs.head;
+  uint4 w[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int at = threadIdx.x + i * kRowThreads;
+    if (at < rs.pieces) w[i] = ld_stream(xi + at * N);
   }
-  for (int i = threadIdx.x; i < rs.pieces; i += kThreads) {
-    float z[N];
-    piece_get<T>(*reinterpret_cast<const uint4*>(x + rs.head + i * N), z);
-    add(z, N);
+  const float ze = edge >= 0 ? Elem<T>::get(x[edge]) : -INFINITY;
+  const float xy = threadIdx.x == 0 && k.valid(p.vocab) ? Elem<T>::get(x[k.y]) : 0.f;
+  if (!k.valid(p.vocab) && threadIdx.x == 0 && p.status) atomicOr(p.status, FE_ST_INDEX);
+  MaxSum v = {ze, 0.f};
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (threadIdx.x + i * kRowThreads < rs.pieces) v.m = piece_max<T>(w[i], v.m);
+  const uint64_t c2 = f32x2_pack(p.c, p.c);
+  {
+    const uint64_t nb = f32x2_pack(-base_of(v.m), -base_of(v.m));
+    uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (threadIdx.x + i * kRowThreads < rs.pieces) piece_sum<T>(w[i], nb, c2, sum);
+    v.s = sum_of(sum) + ex2_approx((ze - base_of(v.m)) * p.c);
   }
-  for (int i = rs.head + rs.pieces * N + threadIdx.x; i < p.vocab; i += kThreads) {
-    const float z = Elem<T>::get(x[i]);
-    add(&z, 1);
-  }
-  v = block_join(v, p.c, sh);
-  if (threadIdx.x == 0) s_k = row_outputs(p, t, k, s_xy, v);
+  v = block_join<kRowThreads>(v, p.c, sh);
+  if (threadIdx.x == 0) s_k = row_outputs(p, t, k, xy, v, true);
+  if (!g) return;
   __syncthreads();
-  if (g) grad_row(x, g, p.vocab, k.y, s_k, p.c, base_of(v.m), 1.f / v.s);
+  const float kf = s_k, f = -kf * (1.f / v.s), b = base_of(v.m);
+  const uint64_t nb = f32x2_pack(-b, -b);
+  T* gi = g + rs.head;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int at = threadIdx.x + i * kRowThreads;
+    if (at < rs.pieces) *reinterpret_cast<uint4*>(gi + at * N) = piece_grad<T>(w[i], nb, c2, f, kf, k.y - rs.head - at * N);
+  }
+  if (edge >= 0) g[edge] = Elem<T>::put(fmaf(f, ex2_approx((ze - b) * p.c), edge == k.y ? kf : 0.f));
+}
+
+// ---------------------------------------------------------------------------
+// long rows: shared memory and L2
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void peer_put(const MaxSum* place, uint32_t rank, MaxSum v) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(place)), "r"(rank));
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(v.m), "f"(v.s) : "memory");
+}
+
+__device__ __forceinline__ uint4 ld_hint(const void* p, uint64_t policy) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0,%1,%2,%3}, [%4], %5;"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p), "l"(policy)
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_hint(void* p, const uint4& v, uint64_t policy) {
+  asm volatile("st.global.L2::cache_hint.v4.u32 [%0], {%1,%2,%3,%4}, %5;" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w),
+               "l"(policy)
+               : "memory");
+}
+
+// cs CTAs (a cluster) share a row; each thread keeps its first `keep` pieces, THREADS apart, and has AHEAD in flight
+template <typename T, int THREADS, int MINB, int AHEAD>
+__global__ void __launch_bounds__(THREADS, MINB) policy_kernel(const PolicyParams p, int cs, int keep) {
+  constexpr int N = Elem<T>::N;
+  extern __shared__ __align__(16) uint4 held[];  // [keep][THREADS]
+  __shared__ MaxSum sh[THREADS / 32];
+  __shared__ __align__(8) MaxSum s_peers[8];
+  uint64_t hold, leave;  // L2's eviction priorities
+  asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(hold));
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(leave));
+  pdl_trigger();
+  if (cs > 1) {  // no peer writes statistics into a CTA that has not begun
+    cluster_arrive();
+    cluster_wait();
+  }
+  pdl_wait();
+  const int lane = threadIdx.x & 31, rank = (int)blockIdx.x % cs, t = (int)blockIdx.x / cs;
+  const Token k = token_of(p, t);
+  const T* x = reinterpret_cast<const T*>(p.logits) + (long long)t * p.logits_row;
+  T* g = p.grad ? reinterpret_cast<T*>(p.grad) + (long long)t * p.grad_row : nullptr;
+  const RowSplit<T> rs(x, p.vocab);
+  const int per = (rs.pieces + cs - 1) / cs, from = min(rank * per, rs.pieces), n = min(from + per, rs.pieces) - from;
+  const int edge = rank == 0 ? edge_of(threadIdx.x, rs, p.vocab) : -1;
+  const T* xi = x + rs.head + (long long)from * N;
+  T* gi = g + rs.head + (long long)from * N;
+  const bool aligned = ((reinterpret_cast<uintptr_t>(xi) ^ reinterpret_cast<uintptr_t>(gi)) & 15u) == 0;
+  auto store = [&](int i, const uint4& w) {
+    if (aligned) {
+      st_hint(gi + i * N, w, leave);
+    } else {
+      const T* e = reinterpret_cast<const T*>(&w);
+#pragma unroll
+      for (int j = 0; j < N; ++j) gi[i * N + j] = e[j];
+    }
+  };
+  if (!k.kept()) {
+    if (threadIdx.x == 0 && rank == 0) p.terms[t] = p.logp[t] = p.lse[t] = p.coef[t] = 0.f;
+    if (g) {
+      for (int i = threadIdx.x; i < n; i += THREADS) store(i, make_uint4(0u, 0u, 0u, 0u));
+      if (edge >= 0) g[edge] = Elem<T>::put(0.f);
+    }
+    return;  // (the whole cluster)
+  }
+  if (!k.valid(p.vocab) && rank == 0 && threadIdx.x == 0 && p.status) atomicOr(p.status, FE_ST_INDEX);
+  const T xy = x[k.valid(p.vocab) ? k.y : 0], xe = x[edge >= 0 ? edge : 0];
+  const uint64_t c2 = f32x2_pack(p.c, p.c);
+  MaxSum v = {-INFINITY, 0.f};
+  const int kn = keep * THREADS;
+  for (int i0 = threadIdx.x; i0 < n; i0 += AHEAD * THREADS) {
+    uint4 w[AHEAD];
+#pragma unroll
+    for (int z = 0; z < AHEAD; ++z)
+      if (i0 + z * THREADS < n) w[z] = ld_hint(xi + (i0 + z * THREADS) * N, i0 + z * THREADS < kn ? leave : hold);
+#pragma unroll
+    for (int z = 0; z < AHEAD; ++z)
+      if (i0 + z * THREADS < min(n, kn)) held[i0 + z * THREADS] = w[z];
+    float m = v.m;
+#pragma unroll
+    for (int z = 0; z < AHEAD; ++z)
+      if (i0 + z * THREADS < n) m = piece_max<T>(w[z], m);
+    const uint64_t nb = f32x2_pack(-base_of(m), -base_of(m));
+    uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+    for (int z = 0; z < AHEAD; ++z)
+      if (i0 + z * THREADS < n) piece_sum<T>(w[z], nb, c2, sum);
+    v.s = rebase(v.s, v.m, m, p.c) + sum_of(sum);
+    v.m = m;
+  }
+  const float ze = edge >= 0 ? Elem<T>::get(xe) : -INFINITY;
+  v = join(v, MaxSum{ze, ze == -INFINITY ? 0.f : 1.f}, p.c);
+  v = block_join<THREADS>(v, p.c, sh);
+  if (cs > 1) {
+    if (threadIdx.x < cs) peer_put(&s_peers[rank], threadIdx.x, v);
+    cluster_arrive();
+    cluster_wait();
+    v = lane < cs ? s_peers[lane] : MaxSum{-INFINITY, 0.f};
+    v = warp_join<32>(v, p.c);
+  }
+  const float kf = row_outputs(p, t, k, Elem<T>::get(xy), v, rank == 0 && threadIdx.x == 0);
+  if (!g) return;
+  const float f = -kf * (1.f / v.s), b = base_of(v.m);
+  const uint64_t nb = f32x2_pack(-b, -b);
+  const int y0 = k.y - rs.head - from * N;
+  for (int i0 = threadIdx.x + kn; i0 < n; i0 += AHEAD * THREADS) {
+    uint4 w[AHEAD];
+#pragma unroll
+    for (int z = 0; z < AHEAD; ++z)
+      if (i0 + z * THREADS < n) w[z] = ld_hint(xi + (i0 + z * THREADS) * N, leave);
+#pragma unroll
+    for (int z = 0; z < AHEAD; ++z) {
+      const int i = i0 + z * THREADS;
+      if (i < n) store(i, piece_grad<T>(w[z], nb, c2, f, kf, y0 - i * N));
+    }
+  }
+#pragma unroll 2
+  for (int i = threadIdx.x; i < min(n, kn); i += THREADS) store(i, piece_grad<T>(held[i], nb, c2, f, kf, y0 - i * N));
+  if (edge >= 0) g[edge] = Elem<T>::put(fmaf(f, ex2_approx((ze - b) * p.c), edge == k.y ? kf : 0.f));
 }
 
 // The gradient from a saved lse and coef
@@ -188,11 +441,11 @@ __global__ void __launch_bounds__(kThreads) policy_backward_kernel(const PolicyP
   const int t = blockIdx.x;
   const Token k = token_of(p, t);
   T* g = reinterpret_cast<T*>(p.grad) + (long long)t * p.grad_row;
-  if (!k.kept) {
-    zero_row(g, p.vocab);
+  if (!k.kept()) {
+    zero_row<kThreads>(g, p.vocab);
     return;
   }
-  if (!k.valid && threadIdx.x == 0 && p.status) atomicOr(p.status, FE_ST_INDEX);
+  if (!k.valid(p.vocab) && threadIdx.x == 0 && p.status) atomicOr(p.status, FE_ST_INDEX);
   const T* x = reinterpret_cast<const T*>(p.logits) + (long long)t * p.logits_row;
   const float f = __ldg(p.coef + t) * p.scale * p.inv_t * (p.upstream ? __ldg(p.upstream) : 1.f);
   grad_row(x, g, p.vocab, k.y, f, p.c, __ldg(p.lse + t) * p.t, 1.f);
@@ -215,6 +468,62 @@ __global__ void __launch_bounds__(1024) policy_sum_kernel(const float* terms, in
     for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     if (threadIdx.x == 0) *loss = (float)s;
   }
+}
+
+constexpr int kKeepLong = 8, kKeepShort = 13;  // pieces a thread keeps: 64 KB of 512 threads, 52 KB of 256
+template <typename T>
+cudaError_t allow_smem() {
+  cudaError_t e = cudaFuncSetAttribute((const void*)policy_kernel<T, 512, 3, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       kKeepLong * 512 * 16);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute((const void*)policy_kernel<T, 256, 4, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             kKeepShort * 256 * 16);
+  return e;
+}
+struct Device {
+  int sms = 0;
+  cudaError_t err = cudaErrorUnknown;
+};
+// Once per device: its SMs and the kernels' shared-memory limits.
+const Device& device() {
+  static Device devs[64];
+  static std::once_flag once[64];
+  static const Device none;
+  int d = 0;
+  if (cudaGetDevice(&d) != cudaSuccess || d < 0 || d >= 64) return none;
+  std::call_once(once[d], [d] {
+    Device& v = devs[d];
+    v.err = cudaDeviceGetAttribute(&v.sms, cudaDevAttrMultiProcessorCount, d);
+    for (cudaError_t (*f)() : {allow_smem<__nv_bfloat16>, allow_smem<__half>, allow_smem<float>})
+      if (v.err == cudaSuccess) v.err = f();
+  });
+  return devs[d];
+}
+
+template <typename T>
+cudaError_t policy_go(const PolicyParams& p, cudaStream_t s) {
+  constexpr int N = Elem<T>::N;
+  const Device& dev = device();
+  if (dev.err != cudaSuccess) return dev.err;
+  const int pieces = (p.vocab + N - 1) / N;
+  // a gradient whose rows start elsewhere between two 16-byte boundaries cannot leave in 16-byte pieces
+  const bool aligned = !p.grad || ((((uintptr_t)p.grad ^ (uintptr_t)p.logits) & 15) == 0 && (p.grad_row - p.logits_row) % N == 0);
+  if (aligned && pieces <= kRowThreads * 8) {
+    const dim3 g((unsigned)p.rows), b(kRowThreads);
+    if (pieces <= kRowThreads) return launch_k(policy_row_kernel<T, 1>, g, b, 0, s, p);
+    if (pieces <= kRowThreads * 2) return launch_k(policy_row_kernel<T, 2>, g, b, 0, s, p);
+    if (pieces <= kRowThreads * 4) return launch_k(policy_row_kernel<T, 4>, g, b, 0, s, p);
+    return launch_k(policy_row_kernel<T, 8>, g, b, 0, s, p);
+  }
+  // few rows: several CTAs each, as long as every thread has a piece
+  int cs = 1;
+  while (cs < 8 && (long long)p.rows * cs < 2 * dev.sms && pieces >= cs * 1024) cs *= 2;
+  const int per = (pieces + cs - 1) / cs;
+  auto go = [&](auto kern, int threads, int most) {
+    const int keep = !p.grad ? 0 : std::min(most, (per + threads - 1) / threads);
+    return launch_kc(kern, dim3((unsigned)(p.rows * cs)), dim3((unsigned)threads), (size_t)keep * threads * 16, s, cs, p, cs, keep);
+  };
+  return per <= 4096 ? go(policy_kernel<T, 256, 4, 4>, 256, kKeepShort) : go(policy_kernel<T, 512, 3, 2>, 512, kKeepLong);
 }
 
 int check_policy(const fe_policy_args* a) {
@@ -280,11 +589,8 @@ extern "C" int fe_policy_loss(const fe_policy_args* a, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const PolicyParams p = policy_params(a, nullptr);
   cudaError_t e = cudaSuccess;
-  const dim3 g((unsigned)a->rows), b(kThreads);
   if (a->rows > 0)
-    e = a->dtype == FE_IO_F32    ? launch_k(policy_kernel<float>, g, b, 0, s, p)
-        : a->dtype == FE_IO_BF16 ? launch_k(policy_kernel<__nv_bfloat16>, g, b, 0, s, p)
-                                 : launch_k(policy_kernel<__half>, g, b, 0, s, p);
+    e = a->dtype == FE_IO_F32 ? policy_go<float>(p, s) : a->dtype == FE_IO_BF16 ? policy_go<__nv_bfloat16>(p, s) : policy_go<__half>(p, s);
   if (e == cudaSuccess) e = launch_k(policy_sum_kernel, dim3(1), dim3(1024), 0, s, (const float*)a->terms, a->rows, a->loss);
   return e == cudaSuccess ? FE_OK : fail_cuda(e, "fe_policy_loss");
 }
