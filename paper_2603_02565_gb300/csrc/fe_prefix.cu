@@ -86,7 +86,7 @@ __device__ __forceinline__ int seen_rows(int len, int n, int j) { return max(0, 
 // ---------------------------------------------------------------------------
 // plan
 // ---------------------------------------------------------------------------
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 1024, kPlanGroups = 4096;
 
 // inclusive sum over the block's threads
 template <typename V>
@@ -130,17 +130,26 @@ __device__ __forceinline__ int find_last(const V* a, int n, V x) {
 __global__ void __launch_bounds__(kPlanThreads) prefix_plan_kernel(const PrefixParams p) {
   __shared__ long long sh[32];
   __shared__ int sh_i[32];
+  __shared__ int sh_groups[kPlanGroups];
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x;
   // offsets that are not increasing from 0 to their ends would send rows nowhere
   bool bad = p.row_start[0] != 0 || p.row_start[p.n_seqs] != p.n_rows || p.group_start[0] != 0 ||
              p.group_start[p.n_groups] != p.n_seqs;
+#pragma unroll 4
   for (int s = tid; s < p.n_seqs; s += kPlanThreads) bad |= p.row_start[s] > p.row_start[s + 1];
   for (int g = tid; g < p.n_groups; g += kPlanThreads) bad |= p.group_start[g] > p.group_start[g + 1];
   bad = __syncthreads_or(bad);
   if (tid == 0) *p.head = PlanHead{0, bad ? 1 : 0, 0, 0};
   if (bad) return;
+  // (the groups' first sequences are searched for every sequence: in shared memory, if they fit)
+  const int32_t* groups = p.group_start;
+  if (p.n_groups <= kPlanGroups) {
+    for (int g = tid; g < p.n_groups; g += kPlanThreads) sh_groups[g] = p.group_start[g];
+    groups = sh_groups;
+    __syncthreads();
+  }
   // row tiles of the groups
   int base = 0;
   for (int g0 = 0; g0 < p.n_groups; g0 += kPlanThreads) {
@@ -169,10 +178,11 @@ __global__ void __launch_bounds__(kPlanThreads) prefix_plan_kernel(const PrefixP
     const int j = min(n - 1, (int)(((long long)(i + 1) * kUnitRows - 1) / p.hr) - (a - first));
     return len_ok(p, len) ? (seen_rows(len, n, j) + kSlot - 1) / kSlot : 0;
   };
+#pragma unroll 4
   for (int s = tid; s < p.n_seqs; s += kPlanThreads) {
     const int a = p.row_start[s], n = p.row_start[s + 1] - a;
     if (n == 0) continue;
-    const int g = find_last(p.group_start, p.n_groups, s), first = p.row_start[p.group_start[g]];
+    const int g = find_last(groups, p.n_groups, s), first = p.row_start[groups[g]];
     const int i = (int)((long long)(a - first) * p.hr / kUnitRows);
     const int c = slots(s, a, n, first, i);
     if (c) atomicAdd(p.cost + p.gtile[g] + i, c);
@@ -286,17 +296,18 @@ struct Ring {
   }
 };
 
-// maximum of 64 values, in four chains
-__device__ __forceinline__ float max64(const float* v) {
+// maximum of N values, in four chains
+template <int N>
+__device__ __forceinline__ float maxn(const float* v) {
   float a[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-  for (int i = 4; i + 8 <= 64; i += 8) {
+  for (int i = 4; i + 8 <= N; i += 8) {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       asm("max.f32 %0, %1, %2, %3;" : "=f"(a[k]) : "f"(a[k]), "f"(v[i + 2 * k]), "f"(v[i + 2 * k + 1]));
   }
-  a[0] = fmaxf(fmaxf(a[0], v[60]), v[61]);
-  a[1] = fmaxf(fmaxf(a[1], v[62]), v[63]);
+  a[0] = fmaxf(fmaxf(a[0], v[N - 4]), v[N - 3]);
+  a[1] = fmaxf(fmaxf(a[1], v[N - 2]), v[N - 1]);
   return fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
 }
 
@@ -363,19 +374,31 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       Ring<2> ur;
       bool ok = true;
       SplitRec rec = {};
-      while (ok && x < hi) {
-        // the unit that holds tile x: group, head, row tile
-        const int g = find_last(p.gcost, p.n_groups + 1, x);
+      // the unit that holds tile x: group, head, row tile; the next ones follow step by step
+      int g = 0, head = 0, ti = 0, off = 0, first_rt = 0, n_rt = 0, s0 = 0, s1 = 0, t0 = 0, group_rows = 0, plen = 0;
+      auto open_group = [&]() {
+        first_rt = p.gtile[g];
+        n_rt = p.gtile[g + 1] - first_rt;
+        s0 = p.group_start[g];
+        s1 = p.group_start[g + 1];
+        plen = prefix_ok(p, p.prefix_len[g]) ? p.prefix_len[g] : 0;
+        t0 = p.row_start[s0];
+        group_rows = (int)min(0x7fffffffLL, (long long)(p.row_start[s1] - t0) * p.hr);
+      };
+      if (x < hi) {
         // (groups without rows have no tiles: the last of equal starts is the one with some)
-        const int first_rt = p.gtile[g], n_rt = p.gtile[g + 1] - first_rt;
+        g = find_last(p.gcost, p.n_groups + 1, x);
+        open_group();
         const long long per_head = (p.gcost[g + 1] - p.gcost[g]) / p.hkv, rem = x - p.gcost[g];
-        const int head = (int)(rem / per_head);
+        head = (int)(rem / per_head);
         const long long y = rem - (long long)head * per_head + p.before[first_rt];
-        const int ti = find_last(p.before + first_rt, n_rt, y), rt = first_rt + ti;
-        const int cost = p.cost[rt], off = (int)(y - p.before[rt]);
+        ti = find_last(p.before + first_rt, n_rt, y);
+        off = (int)(y - p.before[first_rt + ti]);
+      }
+      while (ok && x < hi) {
+        const int cost = p.cost[first_rt + ti];
         const int n = (int)min((long long)(cost - off), hi - x);
-        const int s0 = p.group_start[g], s1 = p.group_start[g + 1], t0 = p.row_start[s0];
-        const int r0 = ti * kUnitRows, rows = (int)min((long long)kUnitRows, (long long)(p.row_start[s1] - t0) * p.hr - r0);
+        const int r0 = ti * kUnitRows, rows = min(kUnitRows, group_rows - r0);
         const int both = rows > 128;
         const int piece = off == 0 && n == cost ? -1 : off == 0 ? 1 : 0;
         if (piece == 1) {  // further pieces: the CTAs that begin inside the unit
@@ -390,7 +413,6 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         mbar_arrive_lane0(u_full + ur.i);
         const int entry = ur.i;
         ur.next();
-        const int plen = prefix_ok(p, p.prefix_len[g]) ? p.prefix_len[g] : 0;
         const int ptiles = (plen + kTileKeys - 1) / kTileKeys;
         // own keys: the sequences of the unit's rows, 32 at a time, with their first slots
         const int ta = t0 + r0 / p.hr, tb = t0 + (r0 + rows - 1) / p.hr;
@@ -520,6 +542,18 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
                            v_full + vr.i, go);
           vr.next();
         }
+        // the next unit: row tile, head, group with rows
+        off = 0;
+        if (x < hi && ++ti == n_rt) {
+          ti = 0;
+          if (++head == p.hkv) {
+            head = 0;
+            do {
+              ++g;
+            } while (p.gtile[g + 1] == p.gtile[g]);
+            open_group();
+          }
+        }
       }
       if (ok && mbar_wait_ok(d_empty + dr.i, dr.par ^ 1u, status)) {
         if (lane == 0) descs[dr.i].flags = TD_END;
@@ -545,82 +579,112 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       Ring<NK> kr;
       Ring<NV> vr;
       Ring<ND> dr;
-      uint32_t qpar[2] = {0, 0};
-      // jobs whose product with V is still to come, oldest first
+      // A group's job whose product with V is still to come (slots 0: none), and how many it has finished
       struct Job {
-        int w, slots, first, release, vi;
-        uint32_t vpar;
-      } q[2];
-      int pending = 0;
-      uint32_t jobs[2] = {0, 0};  // finished jobs of a group
-      bool opened[2] = {false, false};
-      int jp = 0;
-      bool ok = true;
-      auto finish = [&]() {  // O += P V of the oldest job
-        const Job& b = q[0];
-        const int w = b.w;
-        if (!mbar_wait_ok(p_full + w, jobs[w] & 1u, status) || !mbar_wait_ok(v_ready + b.vi, b.vpar, status)) return false;
+        int slots, first, release, vi;
+        uint32_t vpar, done;
+      };
+      Job a = {}, b = {};
+      uint32_t qpars = 0;                 // parities of the query entries, bit e
+      int opened = 0;                     // groups with a product in this unit's output, bit w
+      int flags = 0, slots = 0, entry = 0;  // the tile in hand; left: jobs it still has
+      int left = 0;
+      bool ok = true, end = false;
+      auto finish = [&](Job& b, int w) {  // O += P V of group w's job
+        if (!mbar_wait_ok(p_full + w, b.done & 1u, status) || !mbar_wait_ok(v_ready + b.vi, b.vpar, status)) return false;
         tc_fence_after();
-        const uint32_t o = tmem + C::kO + (uint32_t)(w * D), a = tmem + C::kP + (uint32_t)w * C::kPStep;
+        const uint32_t o = tmem + C::kO + (uint32_t)(w * D), pa = tmem + C::kP + (uint32_t)w * C::kPStep;
         const uint64_t vd = vd0 + (uint64_t)((b.vi * C::kTile) >> 4);
-        for (int s = 0; s < b.slots; ++s)
-          umma_bf16_tmem_a_if(o, a + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv,
-                              s != 0 || !b.first ? 1u : 0u, go);
+        umma_bf16_tmem_a_if(o, pa, vd, idesc_pv, b.first ? 0u : 1u, go);
+        if (b.slots == kSlots) {
+#pragma unroll
+          for (int s = 1; s < kSlots; ++s)
+            umma_bf16_tmem_a_if(o, pa + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv, 1u, go);
+        } else {
+#pragma unroll 1
+          for (int s = 1; s < b.slots; ++s)
+            umma_bf16_tmem_a_if(o, pa + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv, 1u, go);
+        }
         umma_commit_if(pv_done + w, go);
         if (b.release) umma_commit_if(v_empty + b.vi, go);
-        ++jobs[w];
-        q[0] = q[1];
-        --pending;
+        ++b.done;
+        b.slots = 0;
         return true;
       };
-      // What the next job needs may itself wait for a pending one (its queries' space, a stage of V): as long as
-      // it is not there, pending jobs are finished.
-      auto ready = [&](uint64_t* bar, uint32_t par) {
-        while (pending > 0 && !__all_sync(0xffffffffu, mbar_test_wait(bar, par)))
-          if (!finish()) return false;
-        return mbar_wait_ok(bar, par, status);
-      };
-      while (ok) {
-        if (!(ok = ready(d_full + dr.i, dr.par))) break;
-        const TileDesc* td = descs + dr.i;
-        const int flags = td->flags, slots = td->slots, entry = td->entry;
-        if (flags & TD_END) break;
-        mbar_arrive_lane0(d_empty + dr.i);
-        dr.next();
-        const bool both = flags & TD_BOTH;
-        if (flags & TD_FIRST) {
-          if (!(ok = ready(q_full + entry, qpar[entry]))) break;
-          qpar[entry] ^= 1u;
-          opened[0] = opened[1] = false;
+      // The groups take jobs in turn: group w's previous one is finished, then its next one begun, while the other
+      // group's scores are being worked on.  (When the stream has ended, the turns only finish.)
+#pragma unroll 1
+      for (int w = 0; ok; w ^= 1) {
+        Job cur = w ? b : a;
+        if (cur.slots && !(ok = finish(cur, w))) break;
+        if (w)
+          b = cur;
+        else
+          a = cur;
+        if (end) {
+          if (!(w ? a : b).slots) break;
+          continue;
         }
-        if (slots == 0) continue;
-        if (!(ok = ready(k_full + kr.i, kr.par))) break;
-        const uint64_t kd = kd0 + (uint64_t)((kr.i * C::kTile) >> 4);
-        const uint32_t id = idesc | ((uint32_t)(slots * 2) << 17);
-        for (int e = 0; e < (both ? 2 : 1); ++e) {
-          const int w = jp;
-          jp ^= 1;
-          if (pending == 2 && !(ok = finish())) break;
-          // (without columns of its own, P lies where the next S goes)
-          if (!C::kOwnP && jobs[w] > 0 && !(ok = mbar_wait_ok(pv_done + w, (jobs[w] - 1) & 1u, status))) break;
-          tc_fence_after();
-          const uint64_t qd = qd0 + (uint64_t)(((both ? w : entry) * C::kTile) >> 4);
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            const uint64_t at = (uint64_t)(((kk * 32) / C::kRow * C::kHalf + (kk * 32) % C::kRow) >> 4);
-            umma_bf16_if(tmem + C::kS + (uint32_t)(w * 128), qd + at, kd + at, id, kk != 0 ? 1u : 0u, go);
+        while (left == 0) {  // the next tile with keys
+          if (!(ok = mbar_wait_ok(d_full + dr.i, dr.par, status))) break;
+          const TileDesc* td = descs + dr.i;
+          flags = td->flags;
+          slots = td->slots;
+          entry = td->entry;
+          if (flags & TD_END) {
+            end = true;
+            break;
           }
-          umma_commit_if(s_full + w, go);
-          const bool last = !both || e == 1;
-          if (last) umma_commit_if(k_empty + kr.i, go);
-          q[pending++] = Job{w, slots, !opened[w], last, vr.i, vr.par};
-          opened[w] = true;
+          mbar_arrive_lane0(d_empty + dr.i);
+          dr.next();
+          if (flags & TD_FIRST) {
+            // the queries' space may wait for the unit of the other group's job
+            if (!__all_sync(0xffffffffu, mbar_test_wait(q_full + entry, (qpars >> entry) & 1u))) {
+              Job other = w ? a : b;
+              if (other.slots && !(ok = finish(other, w ^ 1))) break;
+              if (w)
+                a = other;
+              else
+                b = other;
+            }
+            if (!(ok = mbar_wait_ok(q_full + entry, (qpars >> entry) & 1u, status))) break;
+            qpars ^= 1u << entry;
+            opened = 0;
+          }
+          if (slots == 0) continue;
+          if (!(ok = mbar_wait_ok(k_full + kr.i, kr.par, status))) break;
+          left = flags & TD_BOTH ? 2 : 1;
         }
         if (!ok) break;
-        kr.next();
-        vr.next();
+        if (end) {
+          if (!(w ? a : b).slots) break;
+          continue;
+        }
+        // (without columns of its own, P lies where the next S goes)
+        if (!C::kOwnP && cur.done > 0 && !(ok = mbar_wait_ok(pv_done + w, (cur.done - 1) & 1u, status))) break;
+        tc_fence_after();
+        const uint64_t qd = qd0 + (uint64_t)(((flags & TD_BOTH ? w : entry) * C::kTile) >> 4);
+        const uint64_t kd = kd0 + (uint64_t)((kr.i * C::kTile) >> 4);
+        const uint32_t id = idesc | ((uint32_t)(slots * 2) << 17);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint64_t at = (uint64_t)(((kk * 32) / C::kRow * C::kHalf + (kk * 32) % C::kRow) >> 4);
+          umma_bf16_if(tmem + C::kS + (uint32_t)(w * 128), qd + at, kd + at, id, kk != 0 ? 1u : 0u, go);
+        }
+        umma_commit_if(s_full + w, go);
+        --left;
+        if (left == 0) umma_commit_if(k_empty + kr.i, go);
+        cur = Job{slots, (opened >> w) & 1 ? 0 : 1, left == 0, vr.i, vr.par, cur.done};
+        opened |= 1 << w;
+        if (w)
+          b = cur;
+        else
+          a = cur;
+        if (left == 0) {
+          kr.next();
+          vr.next();
+        }
       }
-      while (ok && pending > 0) ok = finish();
       umma_drain(drain, status, go);
     } else if (warp == 2) {
       // ---------------- values ----------------
@@ -640,25 +704,23 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         if (slots > 0) {
           if (!mbar_wait_ok(v_full + vr.i, vr.par, status)) break;
           uint8_t* v = sV + vr.i * C::kTile;
-          if (clean) {
-            for (int s = 0; s < slots; ++s) {
-              const int n = __shfl_sync(0xffffffffu, count, s);
-              // (whole rows: the swizzle moves pieces within a row)
-              for (int hf = 0; hf < C::NH; ++hf)
-                for (uint32_t o = (uint32_t)n * C::kRow + lane * 16; o < kSlot * C::kRow; o += 512)
-                  *reinterpret_cast<uint4*>(v + hf * C::kHalf + s * kSlot * C::kRow + o) = make_uint4(0u, 0u, 0u, 0u);
-            }
-            __syncwarp();
-          }
           if (flags & TD_SCAN) {
-            // 0 x as long as every x is a number, NaN from the first other one on
+            // one pass: rows past a slot's end cleared, the others' 0 x summed: 0 as long as every x is a number
             uint32_t acc = 0;
+#pragma unroll
             for (int hf = 0; hf < C::NH; ++hf)
 #pragma unroll 4
               for (uint32_t o = lane * 16; o < (uint32_t)slots * kSlot * C::kRow; o += 512) {
-                const uint4 x = *reinterpret_cast<const uint4*>(v + hf * C::kHalf + o);
-                acc = Elem<T>::zero_fma(x.x, Elem<T>::zero_fma(x.y, Elem<T>::zero_fma(x.z, Elem<T>::zero_fma(x.w, acc))));
+                const uint32_t r = o / C::kRow;
+                uint4* x = reinterpret_cast<uint4*>(v + hf * C::kHalf + o);
+                if ((int)(r % kSlot) >= __shfl_sync(0xffffffffu, count, r / kSlot)) {
+                  *x = make_uint4(0u, 0u, 0u, 0u);
+                } else {
+                  const uint4 y = *x;
+                  acc = Elem<T>::zero_fma(y.x, Elem<T>::zero_fma(y.y, Elem<T>::zero_fma(y.z, Elem<T>::zero_fma(y.w, acc))));
+                }
               }
+            __syncwarp();
             if (__any_sync(0xffffffffu, (acc & 0x7fff7fffu) != 0)) {
               for (int s = 0; s < slots; ++s) {
                 bool found = false;
@@ -681,6 +743,14 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
                   }
                 }
               }
+            }
+          } else if (clean) {
+            for (uint32_t left = (uint32_t)clean; left; left &= left - 1) {
+              const int s = __ffs(left) - 1, n = __shfl_sync(0xffffffffu, count, s);
+              // (whole rows: the swizzle moves pieces within a row)
+              for (int hf = 0; hf < C::NH; ++hf)
+                for (uint32_t o = (uint32_t)n * C::kRow + lane * 16; o < kSlot * C::kRow; o += 512)
+                  *reinterpret_cast<uint4*>(v + hf * C::kHalf + s * kSlot * C::kRow + o) = make_uint4(0u, 0u, 0u, 0u);
             }
           }
           fence_async_shared();
@@ -779,30 +849,48 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         if (!mbar_wait_ok(s_full + w, jobs & 1u, status)) break;
         if (active) {
           tc_fence_after();
-          // The keys' second half gives its maximum first and is read again after the first half
-          // (which needs 64 registers, not 128; P's columns may be the first half's).
-          auto half = [&](int c0, float* v) {  // scores of keys c0 .. c0 + 63, unseen ones -inf
-            tmem_ld64(t_s + (uint32_t)c0, v);
-            if (flags & TD_FULL) return;
-            const int bad = td->bad;
+          // Tiles that every row sees whole go through registers in halves; the second half gives its maximum first
+          // and is read again after the first (64 registers, not 128; P's columns may be the first half's).  Others go
+          // by pairs of slots, twice: pairs that no row of the warp sees cost two votes and their zeros in P.
+          const bool whole = flags & TD_FULL;
+          float v[64];
+          float mx;
+          uint32_t pairs = 0;  // with a key that a row of this warp sees
+          auto seen_of = [&](int at) {  // this row's keys of slot `at`
+            const int owner = td->owner[at];
+            const int n = owner == -1 ? td->count[at] : owner == ri.seq ? min(td->count[at], max(0, ri.seen - td->base[at])) : 0;
+            return at < slots ? n : 0;
+          };
+          auto pair = [&](int z) {  // scores of slots 2 z and 2 z + 1 in v[0 .. 31], unseen ones -inf
+            const int n0 = seen_of(2 * z), n1 = seen_of(2 * z + 1);
+            tmem_ld32(t_s + (uint32_t)(32 * z), v);
+            if (!__all_sync(0xffffffffu, n0 == kSlot && n1 == kSlot)) {
 #pragma unroll
-            for (int z = 0; z < kSlots / 2; ++z) {
-              const int at = c0 / kSlot + z, owner = td->owner[at];
-              int n = owner == -1 ? td->count[at] : owner == ri.seq ? min(td->count[at], max(0, ri.seen - td->base[at])) : 0;
-              if (at >= slots) n = 0;
-              spoiled = spoiled || (n > 0 && ((bad >> at) & 1));
-              if (__any_sync(0xffffffffu, n < kSlot)) {
-#pragma unroll
-                for (int i = 0; i < kSlot; ++i)
-                  if (i >= n) v[z * kSlot + i] = -INFINITY;
+              for (int i = 0; i < kSlot; ++i) {
+                if (i >= n0) v[i] = -INFINITY;
+                if (i >= n1) v[kSlot + i] = -INFINITY;
               }
             }
           };
-          float v[64];
-          half(64, v);
-          float mx = max64(v);
-          half(0, v);
-          mx = fmaxf(mx, max64(v)) * sc;
+          if (whole) {
+            tmem_ld64(t_s + 64u, v);
+            mx = maxn<64>(v);
+            tmem_ld64(t_s, v);
+            mx = fmaxf(mx, maxn<64>(v)) * sc;
+          } else {
+            const int bad = td->bad;
+            mx = -INFINITY;
+#pragma unroll 1
+            for (int z = 0; 2 * z < slots; ++z) {
+              const int n0 = seen_of(2 * z), n1 = seen_of(2 * z + 1);
+              if (!__any_sync(0xffffffffu, n0 + n1 > 0)) continue;
+              pairs |= 1u << z;
+              spoiled = spoiled || (n0 > 0 && ((bad >> (2 * z)) & 1)) || (n1 > 0 && ((bad >> (2 * z + 1)) & 1));
+              pair(z);
+              mx = fmaxf(mx, maxn<32>(v));
+            }
+            mx *= sc;
+          }
           constexpr float kSlack = 8.f;
           if (mine == 0) {
             m = mx;
@@ -832,15 +920,13 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           const float ref = m == -INFINITY ? 0.f : m;
           const uint64_t sc2 = f32x2_pack(sc, sc), nm2 = f32x2_pack(-ref, -ref);
           uint64_t sum[2] = {0ull, 0ull};
-#pragma unroll
-          for (int c0 = 0; c0 < 128; c0 += 32) {
-            if (c0 == 64) half(64, v);
+          auto weights = [&](const float* x, int c0) {  // P of 32 keys from column c0 of S on
             uint32_t pk[16];
 #pragma unroll
             for (int i = 0; i < 32; i += 4) {
               float e[4];
-              f32x2_unpack(f32x2_fma(f32x2_pack(v[c0 % 64 + i], v[c0 % 64 + i + 1]), sc2, nm2), e[0], e[1]);
-              f32x2_unpack(f32x2_fma(f32x2_pack(v[c0 % 64 + i + 2], v[c0 % 64 + i + 3]), sc2, nm2), e[2], e[3]);
+              f32x2_unpack(f32x2_fma(f32x2_pack(x[i], x[i + 1]), sc2, nm2), e[0], e[1]);
+              f32x2_unpack(f32x2_fma(f32x2_pack(x[i + 2], x[i + 3]), sc2, nm2), e[2], e[3]);
 #pragma unroll
               for (int z = 0; z < 4; ++z) e[z] = ex2_approx(e[z]);
               uint64_t& acc = sum[(i >> 2) & 1];
@@ -849,6 +935,24 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
               pk[i / 2 + 1] = Elem<T>::put2(e[2], e[3]);
             }
             tmem_st16_nowait(t_p + (uint32_t)(c0 / 2), pk);
+          };
+          if (whole) {
+            weights(v, 0);
+            weights(v + 32, 32);
+            tmem_ld64(t_s + 64u, v);
+            weights(v, 64);
+            weights(v + 32, 96);
+          } else {
+#pragma unroll 1
+            for (int z = 0; 2 * z < slots; ++z) {
+              if ((pairs >> z) & 1) {
+                pair(z);
+                weights(v, 32 * z);
+              } else {
+                const uint32_t zero[16] = {};
+                tmem_st16_nowait(t_p + (uint32_t)(16 * z), zero);
+              }
+            }
           }
           float a0, a1, a2, a3;
           f32x2_unpack(sum[0], a0, a1);
