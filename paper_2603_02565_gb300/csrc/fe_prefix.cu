@@ -404,6 +404,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         if (piece == 1) {  // further pieces: the CTAs that begin inside the unit
           const long long end = x + cost;
           int c = cta + 1;
+#pragma unroll 1
           while (c < ctas && total * c / ctas < end) ++c;
           rec = SplitRec{c - cta - 1, t0, r0, rows, head, {}};
         }
@@ -494,6 +495,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
             b_row = (page * p.hkv + head) * p.page_rows + (b_base - col * p.page_rows);
           }
         };
+#pragma unroll 1
         for (int j = off; j < off + n; ++j, ++x) {
           const int part = j >= ptiles;
           if (b_part != part || j >= b_first + 4) batch(j, part);
@@ -589,7 +591,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       int opened = 0;                     // groups with a product in this unit's output, bit w
       int flags = 0, slots = 0, entry = 0;  // the tile in hand; left: jobs it still has
       int left = 0;
-      bool ok = true, end = false;
+      bool ok = true, end = false, new_tile = true;
       auto finish = [&](Job& b, int w) {  // O += P V of group w's job
         if (!mbar_wait_ok(p_full + w, b.done & 1u, status) || !mbar_wait_ok(v_ready + b.vi, b.vpar, status)) return false;
         tc_fence_after();
@@ -612,7 +614,9 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         return true;
       };
       // The groups take jobs in turn: group w's previous one is finished, then its next one begun, while the other
-      // group's scores are being worked on.  (When the stream has ended, the turns only finish.)
+      // group's scores are being worked on.
+      bool need_q = false;  // the tile in hand opens a unit whose queries have not been waited for
+      int due = 0;          // the group that takes the next job
 #pragma unroll 1
       for (int w = 0; ok; w ^= 1) {
         Job cur = w ? b : a;
@@ -621,11 +625,9 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           b = cur;
         else
           a = cur;
-        if (end) {
-          if (!(w ? a : b).slots) break;
-          continue;
-        }
-        while (left == 0) {  // the next tile with keys
+        const bool other = (w ? a : b).slots != 0;
+        if (w != due) continue;
+        while (left == 0 && !end && !need_q) {  // the next tile
           if (!(ok = mbar_wait_ok(d_full + dr.i, dr.par, status))) break;
           const TileDesc* td = descs + dr.i;
           flags = td->flags;
@@ -637,29 +639,31 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           }
           mbar_arrive_lane0(d_empty + dr.i);
           dr.next();
-          if (flags & TD_FIRST) {
-            // the queries' space may wait for the unit of the other group's job
-            if (!__all_sync(0xffffffffu, mbar_test_wait(q_full + entry, (qpars >> entry) & 1u))) {
-              Job other = w ? a : b;
-              if (other.slots && !(ok = finish(other, w ^ 1))) break;
-              if (w)
-                a = other;
-              else
-                b = other;
-            }
-            if (!(ok = mbar_wait_ok(q_full + entry, (qpars >> entry) & 1u, status))) break;
-            qpars ^= 1u << entry;
-            opened = 0;
-          }
-          if (slots == 0) continue;
-          if (!(ok = mbar_wait_ok(k_full + kr.i, kr.par, status))) break;
-          left = flags & TD_BOTH ? 2 : 1;
+          need_q = flags & TD_FIRST;
+          if (!need_q && slots) left = flags & TD_BOTH ? 2 : 1;
         }
         if (!ok) break;
         if (end) {
-          if (!(w ? a : b).slots) break;
+          if (!other) break;
           continue;
         }
+        if (need_q) {
+          // (the queries' space may wait for the unit of the other group's job: that is finished first)
+          const uint32_t par = (qpars >> entry) & 1u;
+          if (other && !__all_sync(0xffffffffu, mbar_test_wait(q_full + entry, par))) continue;
+          if (!(ok = mbar_wait_ok(q_full + entry, par, status))) break;
+          qpars ^= 1u << entry;
+          opened = 0;
+          need_q = false;
+          if (slots == 0) {
+            w ^= 1;  // (the same turn again)
+            continue;
+          }
+          left = flags & TD_BOTH ? 2 : 1;
+        }
+        due ^= 1;
+        if (new_tile && !(ok = mbar_wait_ok(k_full + kr.i, kr.par, status))) break;
+        new_tile = false;
         // (without columns of its own, P lies where the next S goes)
         if (!C::kOwnP && cur.done > 0 && !(ok = mbar_wait_ok(pv_done + w, (cur.done - 1) & 1u, status))) break;
         tc_fence_after();
@@ -683,6 +687,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         if (left == 0) {
           kr.next();
           vr.next();
+          new_tile = true;
         }
       }
       umma_drain(drain, status, go);
@@ -707,9 +712,9 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           if (flags & TD_SCAN) {
             // one pass: rows past a slot's end cleared, the others' 0 x summed: 0 as long as every x is a number
             uint32_t acc = 0;
-#pragma unroll
+#pragma unroll 1
             for (int hf = 0; hf < C::NH; ++hf)
-#pragma unroll 4
+#pragma unroll 2
               for (uint32_t o = lane * 16; o < (uint32_t)slots * kSlot * C::kRow; o += 512) {
                 const uint32_t r = o / C::kRow;
                 uint4* x = reinterpret_cast<uint4*>(v + hf * C::kHalf + o);
@@ -722,9 +727,12 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
               }
             __syncwarp();
             if (__any_sync(0xffffffffu, (acc & 0x7fff7fffu) != 0)) {
+#pragma unroll 1
               for (int s = 0; s < slots; ++s) {
                 bool found = false;
+#pragma unroll 1
                 for (int hf = 0; hf < C::NH; ++hf)
+#pragma unroll 1
                   for (uint32_t o = lane * 2; o < kSlot * C::kRow; o += 64) {
                     T* x = reinterpret_cast<T*>(v + hf * C::kHalf + s * kSlot * C::kRow + o);
                     const float f = Elem<T>::get(*x) * 0.f;
@@ -745,6 +753,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
               }
             }
           } else if (clean) {
+#pragma unroll 1
             for (uint32_t left = (uint32_t)clean; left; left &= left - 1) {
               const int s = __ffs(left) - 1, n = __shfl_sync(0xffffffffu, count, s);
               // (whole rows: the swizzle moves pieces within a row)
@@ -787,6 +796,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         constexpr int NP = D / 8, RP = 32 / NP;  // pieces of a row, rows of a step
         const int pc = lane % NP;
         const uint32_t hoff = (uint32_t)(pc * 16) / C::kRow * C::kHalf, poff = (uint32_t)(pc * 16) % C::kRow;
+#pragma unroll 2
         for (int r = lane / NP; r < u.rows; r += RP) {
           const int rr = u.r0 + r, t = u.t0 + rr / p.hr, h = u.head * p.hr + rr % p.hr;
           const T* src = reinterpret_cast<const T*>(p.q) + (long long)t * p.q_row + h * p.q_head + pc * 8;
@@ -794,6 +804,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           const uint32_t mask = C::kRow == 128 ? (row & 7u) : ((row >> 1) & 3u);
           cp_async16(smem_u32(sQ) + (uint32_t)((u.both ? r >> 7 : e) * C::kTile) + hoff + row * C::kRow + (poff ^ (mask << 4)), src);
         }
+#pragma unroll 1
         for (int r = lane; r < n; r += 32) {
           RowInfo ri = {-5, 0, -1, 0};
           if (r < u.rows) {
@@ -820,8 +831,10 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
     const uint32_t t_o = tl + C::kO + (uint32_t)(w * D);
     const float sc = p.sc;
     Ring<ND> dr;
-    uint32_t qpar[2] = {0, 0}, jobs = 0, xs = 0, xr = 0;
-    int jp = 0, mine = 0;  // jobs of this unit
+    uint32_t qpars = 0, jobs0 = 0, jobs1 = 0;  // query entries' parities, bit e; the groups' jobs so far
+    uint32_t joined = 0;                       // units that both groups had a part in
+    bool partner = false;                      // the other group may still be reading this one's output of the last unit
+    int jp = 0, mine0 = 0, mine1 = 0;          // the group that takes the next job; their jobs of this unit
     uint32_t unit = 0;
     RowInfo ri = {-5, 0, -1, 0};
     float m = -INFINITY, l = 0.f;
@@ -834,63 +847,71 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       const bool both = flags & TD_BOTH;
       const int entry = td->entry, piece = td->piece;
       if (flags & TD_FIRST) {
-        if (!mbar_wait_ok(q_full + entry, qpar[entry], status)) break;
-        qpar[entry] ^= 1u;
+        if (!mbar_wait_ok(q_full + entry, (qpars >> entry) & 1u, status)) break;
+        qpars ^= 1u << entry;
+        if (partner && !mbar_wait_ok(x_read + (1 - w) * 4 + qd, (joined - 1) & 1u, status)) break;
+        partner = false;
         ri = rinfo[(both ? w * 128 : entry * 128) + row];
         active = __any_sync(0xffffffffu, ri.seq >= 0);
         m = -INFINITY;
         l = 0.f;
-        mine = 0;
+        mine0 = mine1 = 0;
         spoiled = ri.seen < 0;
       }
-      const bool job = slots > 0 && (both || jp == w);
+      const bool job0 = slots > 0 && (both || jp == 0), job1 = slots > 0 && (both || jp == 1);
       if (slots > 0 && !both) jp ^= 1;
-      if (job) {
+      const uint32_t jobs = w ? jobs1 : jobs0;
+      const int mine = w ? mine1 : mine0;
+      jobs0 += job0, jobs1 += job1;
+      mine0 += job0, mine1 += job1;
+      if (w ? job1 : job0) {
         if (!mbar_wait_ok(s_full + w, jobs & 1u, status)) break;
         if (active) {
           tc_fence_after();
-          // Tiles that every row sees whole go through registers in halves; the second half gives its maximum first
-          // and is read again after the first (64 registers, not 128; P's columns may be the first half's).  Others go
-          // by pairs of slots, twice: pairs that no row of the warp sees cost two votes and their zeros in P.
+          // Scores are read twice, for the maximum and for P, and never held (code and registers: the roles'
+          // instructions compete for the SM's instruction cache).  Tiles that every row sees whole go by halves,
+          // others by pairs of slots, of which those that no row of the warp sees cost their zeros in P.
           const bool whole = flags & TD_FULL;
-          float v[64];
-          float mx;
-          uint32_t pairs = 0;  // with a key that a row of this warp sees
-          auto seen_of = [&](int at) {  // this row's keys of slot `at`
-            const int owner = td->owner[at];
-            const int n = owner == -1 ? td->count[at] : owner == ri.seq ? min(td->count[at], max(0, ri.seen - td->base[at])) : 0;
-            return at < slots ? n : 0;
-          };
-          auto pair = [&](int z) {  // scores of slots 2 z and 2 z + 1 in v[0 .. 31], unseen ones -inf
-            const int n0 = seen_of(2 * z), n1 = seen_of(2 * z + 1);
+          float mx = -INFINITY;
+          uint32_t pairs = 0, seen0 = 0, seen1 = 0;  // pairs with a key that a row of the warp sees; this row's keys of
+                                                     // slots 0 .. 3 and 4 .. 7, a byte each
+          auto pair = [&](int z, float* v) {  // scores of slots 2 z and 2 z + 1, unseen ones -inf
             tmem_ld32(t_s + (uint32_t)(32 * z), v);
-            if (!__all_sync(0xffffffffu, n0 == kSlot && n1 == kSlot)) {
+            const uint32_t two = (z < 2 ? seen0 : seen1) >> (16 * (z & 1));
+            const int n0 = two & 0xff, n1 = (two >> 8) & 0xff;
 #pragma unroll
-              for (int i = 0; i < kSlot; ++i) {
-                if (i >= n0) v[i] = -INFINITY;
-                if (i >= n1) v[kSlot + i] = -INFINITY;
-              }
+            for (int i = 0; i < kSlot; ++i) {
+              if (i >= n0) v[i] = -INFINITY;
+              if (i >= n1) v[kSlot + i] = -INFINITY;
             }
           };
           if (whole) {
-            tmem_ld64(t_s + 64u, v);
-            mx = maxn<64>(v);
-            tmem_ld64(t_s, v);
-            mx = fmaxf(mx, maxn<64>(v)) * sc;
+#pragma unroll 1
+            for (int c0 = 0; c0 < 128; c0 += 64) {
+              float v[64];
+              tmem_ld64(t_s + (uint32_t)c0, v);
+              mx = fmaxf(mx, maxn<64>(v));
+            }
           } else {
             const int bad = td->bad;
-            mx = -INFINITY;
+#pragma unroll
+            for (int at = 0; at < kSlots; ++at) {
+              const int owner = td->owner[at], count = td->count[at];
+              int n = owner == -1 ? count : owner == ri.seq ? min(count, max(0, ri.seen - td->base[at])) : 0;
+              if (at >= slots) n = 0;
+              spoiled = spoiled || (n > 0 && ((bad >> at) & 1));
+              (at < 4 ? seen0 : seen1) |= (uint32_t)n << (8 * (at & 3));
+            }
+            pairs = (__any_sync(0xffffffffu, seen0 & 0xffffu) ? 1u : 0u) | (__any_sync(0xffffffffu, seen0 >> 16) ? 2u : 0u) |
+                    (__any_sync(0xffffffffu, seen1 & 0xffffu) ? 4u : 0u) | (__any_sync(0xffffffffu, seen1 >> 16) ? 8u : 0u);
 #pragma unroll 1
-            for (int z = 0; 2 * z < slots; ++z) {
-              const int n0 = seen_of(2 * z), n1 = seen_of(2 * z + 1);
-              if (!__any_sync(0xffffffffu, n0 + n1 > 0)) continue;
-              pairs |= 1u << z;
-              spoiled = spoiled || (n0 > 0 && ((bad >> (2 * z)) & 1)) || (n1 > 0 && ((bad >> (2 * z + 1)) & 1));
-              pair(z);
+            for (uint32_t left = pairs; left; left &= left - 1) {
+              float v[32];
+              pair(__ffs(left) - 1, v);
               mx = fmaxf(mx, maxn<32>(v));
             }
-            mx *= sc;
           }
+          mx *= sc;
           constexpr float kSlack = 8.f;
           if (mine == 0) {
             m = mx;
@@ -937,16 +958,19 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
             tmem_st16_nowait(t_p + (uint32_t)(c0 / 2), pk);
           };
           if (whole) {
-            weights(v, 0);
-            weights(v + 32, 32);
-            tmem_ld64(t_s + 64u, v);
-            weights(v, 64);
-            weights(v + 32, 96);
+#pragma unroll 1
+            for (int c0 = 0; c0 < 128; c0 += 64) {
+              float v[64];
+              tmem_ld64(t_s + (uint32_t)c0, v);
+              weights(v, c0);
+              weights(v + 32, c0 + 32);
+            }
           } else {
 #pragma unroll 1
             for (int z = 0; 2 * z < slots; ++z) {
               if ((pairs >> z) & 1) {
-                pair(z);
+                float v[32];
+                pair(z, v);
                 weights(v, 32 * z);
               } else {
                 const uint32_t zero[16] = {};
@@ -962,8 +986,6 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           tc_fence_before();
         }
         mbar_arrive_lane0(p_full + w);
-        ++jobs;
-        ++mine;
       }
       mbar_arrive_lane0(d_empty + dr.i);
       dr.next();
@@ -981,118 +1003,82 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         ++unit;
       }
       if (spoiled) l = NAN;
-      if (mine > 0) {
-        if (!mbar_wait_ok(pv_done + w, (jobs - 1) & 1u, status)) break;
-        tc_fence_after();
+      // every S of this group is complete: the unit's queries may go
+      if (both) {
+        mbar_arrive_lane0(q_free);
+        mbar_arrive_lane0(q_free + 1);
+      } else {
+        mbar_arrive_lane0(q_free + entry);
       }
-      float f = 1.f;  // of this group's accumulator
-      float ms = m, ls = l;
-      const int h = both ? 0 : entry;  // the half whose space the exchange takes
+      // Each group reads its own rows' output, or, of rows that both had a part in, half of the columns of both
+      // outputs (a warp's TMEM lanes are its partner's).
+      bool have0 = both ? mine > 0 || (w ? job1 : job0) : mine0 > 0, have1 = !both && mine1 > 0;
+      float f0 = 1.f, f1 = 0.f, ms = m, ls = l;
       if (!both) {
         s_ml[w * 128 + row] = make_float2(m, l);
         mbar_arrive_lane0(x_full + w * 4 + qd);
-        if (!mbar_wait_ok(x_full + (1 - w) * 4 + qd, xr & 1u, status)) break;
-        ++xr;
-        const float2 o = s_ml[(1 - w) * 128 + row];
-        ms = fmaxf(m, o.x);
+        if (!mbar_wait_ok(x_full + (1 - w) * 4 + qd, joined & 1u, status)) break;
+        ++joined;
+        partner = true;
+        const float2 a = s_ml[row], b = s_ml[128 + row];
+        ms = fmaxf(a.x, b.x);
         const float ref = ms == -INFINITY ? 0.f : ms;
-        f = ex2_approx(m - ref);
-        const float fo = ex2_approx(o.x - ref);
-        ls = w == 0 ? fmaf(l, f, o.y * fo) : fmaf(o.y, fo, l * f);
+        f0 = ex2_approx(a.x - ref);
+        f1 = ex2_approx(b.x - ref);
+        ls = fmaf(a.y, f0, b.y * f1);
       }
       const bool store = ri.out >= 0;
-      const float inv = ls == 0.f ? 0.f : 1.f / ls;
-      T* out = reinterpret_cast<T*>(p.out) + (long long)ri.out * D;
+      if (piece < 0) {
+        const float inv = ls == 0.f ? 0.f : 1.f / ls;
+        f0 *= inv;
+        f1 *= inv;
+      }
+      if (have0 && !mbar_wait_ok(pv_done + (both ? w : 0), ((both && w ? jobs1 : jobs0) - 1) & 1u, status)) break;
+      if (have1 && !mbar_wait_ok(pv_done + 1, (jobs1 - 1) & 1u, status)) break;
+      tc_fence_after();
       const long long slot = ((long long)blockIdx.x * 2 + (piece == 1)) * kUnitRows + (both ? w * 128 : 0) + row;
-      // columns c0 .. c0 + N - 1 of the row, summed
-      auto put = [&](auto count, int c0, float* o) {
-        constexpr int N = decltype(count)::value;
-        if (piece < 0) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) o[i] *= inv;
-          if (store) {
-#pragma unroll
-            for (int i = 0; i < N; i += 8) *reinterpret_cast<uint4*>(out + c0 + i) = piece_put<T>(o + i);
-          }
-        } else if (store) {
-#pragma unroll
-          for (int i = 0; i < N; i += 8) st_sector(p.part_o + slot * D + c0 + i, o + i);
-        }
-      };
-      if (both) {
+      T* out = reinterpret_cast<T*>(p.out) + (long long)ri.out * D;
+      float* part = p.part_o + slot * D;
+      const uint32_t t_o0 = both ? t_o : tl + C::kO, t_o1 = tl + C::kO + (uint32_t)D;
+      const int c_end = both ? D : (w + 1) * (D / 2);
 #pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += 32) {
-          float o[32];
-          if (mine > 0) {
-            tmem_ld32(t_o + (uint32_t)c0, o);
-          } else {
+      for (int c0 = both ? 0 : w * (D / 2); c0 < c_end; c0 += 16) {
+        float o[16], o1[16];
+        if (have0) {
+          tmem_ld16(t_o0 + (uint32_t)c0, o);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = 0.f;
-          }
-          put(std::integral_constant<int, 32>(), c0, o);
+          for (int i = 0; i < 16; ++i) o[i] *= f0;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[i] = 0.f;
         }
-      } else {
-        // each group finishes half of the columns; the other half goes to its partner through the unit's query space
-        constexpr int N = D / 4;
-        float* xb = reinterpret_cast<float*>(sQ + h * C::kTile);  // [2][N][128]
-        auto load = [&](int c0, float* o) {
-          if (mine > 0) {
+        if (have1) {
+          tmem_ld16(t_o1 + (uint32_t)c0, o1);
 #pragma unroll
-            for (int i = 0; i < N; i += 8) {
-              uint32_t r8[8];
-              tmem_ld8(t_o + (uint32_t)(c0 + i), r8);
-#pragma unroll
-              for (int z = 0; z < 8; ++z) o[i + z] = __uint_as_float(r8[z]) * f;
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) o[i] = 0.f;
-          }
-        };
-        bool ok = true;
-#pragma unroll 1
-        for (int r = 0; r < 2 && ok; ++r) {
-          float o[N];
-          load((1 - w) * (D / 2) + r * N, o);
-          if (r == 1) ok = mbar_wait_ok(x_read + w * 4 + qd, xs & 1u, status);
-          if (!ok) break;
-#pragma unroll
-          for (int i = 0; i < N; ++i) xb[(w * N + i) * 128 + row] = o[i];
-          mbar_arrive_lane0(x_full + w * 4 + qd);
-          load(w * (D / 2) + r * N, o);
-          ok = mbar_wait_ok(x_full + (1 - w) * 4 + qd, xr & 1u, status);
-          if (!ok) break;
-          ++xr;
-#pragma unroll
-          for (int i = 0; i < N; ++i) o[i] += xb[((1 - w) * N + i) * 128 + row];
-          if (r == 0) mbar_arrive_lane0(x_read + (1 - w) * 4 + qd);
-          put(std::integral_constant<int, N>(), w * (D / 2) + r * N, o);
+          for (int i = 0; i < 16; ++i) o[i] = fmaf(o1[i], f1, o[i]);
         }
-        if (!ok) break;
-        ++xs;
+        if (store) {
+          if (piece < 0) {
+            *reinterpret_cast<uint4*>(out + c0) = piece_put<T>(o);
+            *reinterpret_cast<uint4*>(out + c0 + 8) = piece_put<T>(o + 8);
+          } else {
+            st_sector(part + c0, o);
+            st_sector(part + c0 + 8, o + 8);
+          }
+        }
       }
       tc_fence_before();
-      if (store) {
+      if (!both) mbar_arrive_lane0(x_read + w * 4 + qd);
+      if (store && (both || w == 0)) {
         if (piece < 0) {
-          if (both || w == 0) {
-            if (!(ls == ls)) {
-              const int at = atomicAdd(&p.head->listed, 1);
-              if (at < kListed) p.list[at] = ri.out;
-            }
-            if (p.lse) p.lse[ri.out] = ls == 0.f ? -INFINITY : (ms + log2f(ls)) * 0.693147180559945309f;
+          if (!(ls == ls)) {
+            const int at = atomicAdd(&p.head->listed, 1);
+            if (at < kListed) p.list[at] = ri.out;
           }
-        } else if (both || w == 0) {
+          if (p.lse) p.lse[ri.out] = ls == 0.f ? -INFINITY : (ms + log2f(ls)) * 0.693147180559945309f;
+        } else {
           p.part_ml[slot] = make_float2(ms, ls);
         }
-      }
-      fence_async_shared();
-      // this group is done with the unit's queries, row data and exchange space
-      __syncwarp();
-      if (both) {
-        mbar_arrive_if_at(smem_u32(q_free), lane == 0);
-        mbar_arrive_if_at(smem_u32(q_free + 1), lane == 0);
-      } else {
-        mbar_arrive_if_at(smem_u32(q_free + entry), lane == 0);
       }
     }
   }
