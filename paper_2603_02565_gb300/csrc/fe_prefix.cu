@@ -59,7 +59,7 @@ struct PrefixParams {
   float* lse;
   int32_t* status;
   int64_t q_row, q_head;
-  int n_groups, n_seqs, n_rows, hq, hkv, hr, prefix_cols, page_cols, page_rows, n_pages;
+  int n_groups, n_seqs, n_rows, hq, hkv, hr, prefix_cols, page_cols, page_rows, page_shift, n_pages;
   float scale, sc;  // sc: scale log2(e), and no 0 (masked scores, -inf, are multiplied by it)
   int ctas, max_tiles;
   // workspace
@@ -243,6 +243,11 @@ struct Dirty {
   int n, seq[kDirty];  // n > kDirty: any of them
 };
 
+// Tensor maps of the pages: a slot of 16 rows, and the page or tile, whichever is smaller
+struct PageMaps {
+  CUtensorMap k, v, k_page, v_page;
+};
+
 template <int D>
 struct PrefixCfg {
   static constexpr int kThreads = 384;
@@ -313,8 +318,7 @@ __device__ __forceinline__ float maxn(const float* v) {
 
 template <typename T, int D>
 __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
-    prefix_attend_kernel(const __grid_constant__ CUtensorMap tK, const __grid_constant__ CUtensorMap tV,
-                         const PrefixParams p) {
+    prefix_attend_kernel(const __grid_constant__ PageMaps maps, const PrefixParams p) {
   using C = PrefixCfg<D>;
   constexpr int NK = C::NK, NV = C::NV, ND = C::ND;
   extern __shared__ uint8_t smem_raw[];
@@ -346,8 +350,10 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       mbar_init(q_free + i, 8);
     }
     fence_mbar_init();
-    prefetch_tmap(&tK);
-    prefetch_tmap(&tV);
+    prefetch_tmap(&maps.k);
+    prefetch_tmap(&maps.v);
+    prefetch_tmap(&maps.k_page);
+    prefetch_tmap(&maps.v_page);
   }
   if (warp == 1) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
@@ -362,6 +368,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
     if (warp == 0) {
       // ---------------- schedule and loads ----------------
       const int cta = blockIdx.x;
+      const uint32_t go = elect_one();
       const bool bad_plan = p.head->bad != 0;
       const long long total = bad_plan ? 0 : p.gcost[p.n_groups];
       // (no more CTAs than tiles: each of them has one at least)
@@ -441,22 +448,26 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         // a batch of 32 slots (four tiles) of one part; this lane's slot
         int b_first = -1, b_part = -1;  // first tile of the batch, its part
         int b_owner = 0, b_base = 0, b_count = 0, b_row = 0, b_bad = 0;
+        int ahead = -1, ahead_page = 0;  // the prefix batch whose pages have been asked for, this lane's page
+        const int32_t* pre_table = p.prefix_pages + (long long)g * p.prefix_cols;
         auto batch = [&](int tile, int part) {
           b_first = tile;
           b_part = part;
           b_owner = -2;
           b_base = b_count = b_row = b_bad = 0;
-          const int32_t* table = nullptr;
-          int cols = 0;
+          int page = -1;
           if (part == 0) {
             const int k = (tile * kSlots + lane) * kSlot;
             if (k < plen) {
               b_owner = -1;
               b_base = k;
               b_count = min(kSlot, plen - k);
-              table = p.prefix_pages + (long long)g * p.prefix_cols;
-              cols = p.prefix_cols;
+              page = ahead == tile ? ahead_page : __ldg(pre_table + (k >> p.page_shift));
             }
+            // (nothing is done with the next batch's page before its turn)
+            const int next = k + 32 * kSlot;
+            ahead = tile + 4;
+            if (next < plen) ahead_page = __ldg(pre_table + (next >> p.page_shift));
           } else {
             const int slot = (tile - ptiles) * kSlots + lane;
             if (!own_open) {
@@ -477,22 +488,19 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
                 b_owner = cs + at;
                 b_base = (slot - st) * kSlot;
                 b_count = min(kSlot, seen - b_base);
-                table = p.pages + (long long)b_owner * p.page_cols;
-                cols = p.page_cols;
+                page = __ldg(p.pages + (long long)b_owner * p.page_cols + (b_base >> p.page_shift));
               }
               // past the chunk's end: the next one, as long as its sequences have rows here
               if (!__any_sync(0xffffffffu, b_owner == -2 && slot >= c_end) || cs + 32 >= s1 || p.row_start[cs + 32] > tb) break;
               chunk(cs + 32, c_end);
             }
           }
-          if (table) {
-            const int col = b_base / p.page_rows;
-            int page = col < cols ? __ldg(table + col) : -1;
+          if (b_owner != -2) {
             if (page < 0 || page >= p.n_pages) {
               b_bad = 1;
               page = 0;
             }
-            b_row = (page * p.hkv + head) * p.page_rows + (b_base - col * p.page_rows);
+            b_row = ((page * p.hkv + head) << p.page_shift) + (b_base & (p.page_rows - 1));
           }
         };
 #pragma unroll 1
@@ -526,22 +534,23 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           dr.next();
           if (slots == 0) continue;
           const uint32_t bytes = (uint32_t)slots * kSlot * D * 2;
-          const uint32_t go = mine && b_owner != -2;
-          if (!(ok = mbar_wait_ok(k_empty + kr.i, kr.par ^ 1u, status))) break;
-          mbar_arrive_expect_tx_if(k_full + kr.i, bytes, lane == 0);
-          __syncwarp();
+          const bool whole = slots == kSlots && part == 0 && part_m == 0 && badm == 0;  // pages follow one another
+          const int step = whole ? p.page_rows / kSlot : 1;
+          auto load = [&](uint8_t* dst, const CUtensorMap* map, uint64_t* bar) {
+            mbar_arrive_expect_tx_if(bar, bytes, go);
+#pragma unroll 1
+            for (int i = 0; i < slots; i += step) {
+              const int r = __shfl_sync(0xffffffffu, b_row, l0 + i);
 #pragma unroll
-          for (int hf = 0; hf < C::NH; ++hf)
-            tma_load_2d_if(sK + kr.i * C::kTile + hf * C::kHalf + (lane - l0) * kSlot * C::kRow, &tK, 64 * hf, b_row,
-                           k_full + kr.i, go);
+              for (int hf = 0; hf < C::NH; ++hf)
+                tma_load_2d_if(dst + hf * C::kHalf + i * kSlot * C::kRow, map, 64 * hf, r, bar, go);
+            }
+          };
+          if (!(ok = mbar_wait_ok(k_empty + kr.i, kr.par ^ 1u, status))) break;
+          load(sK + kr.i * C::kTile, whole ? &maps.k_page : &maps.k, k_full + kr.i);
           kr.next();
           if (!(ok = mbar_wait_ok(v_empty + vr.i, vr.par ^ 1u, status))) break;
-          mbar_arrive_expect_tx_if(v_full + vr.i, bytes, lane == 0);
-          __syncwarp();
-#pragma unroll
-          for (int hf = 0; hf < C::NH; ++hf)
-            tma_load_2d_if(sV + vr.i * C::kTile + hf * C::kHalf + (lane - l0) * kSlot * C::kRow, &tV, 64 * hf, b_row,
-                           v_full + vr.i, go);
+          load(sV + vr.i * C::kTile, whole ? &maps.v_page : &maps.v, v_full + vr.i);
           vr.next();
         }
         // the next unit: row tile, head, group with rows
@@ -583,7 +592,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       Ring<ND> dr;
       // A group's job whose product with V is still to come (slots 0: none), and how many it has finished
       struct Job {
-        int slots, first, release, vi;
+        int slots, first, shared, vi;
         uint32_t vpar, done;
       };
       Job a = {}, b = {};
@@ -591,103 +600,113 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       int opened = 0;                     // groups with a product in this unit's output, bit w
       int flags = 0, slots = 0, entry = 0;  // the tile in hand; left: jobs it still has
       int left = 0;
-      bool ok = true, end = false, new_tile = true;
-      auto finish = [&](Job& b, int w) {  // O += P V of group w's job
-        if (!mbar_wait_ok(p_full + w, b.done & 1u, status) || !mbar_wait_ok(v_ready + b.vi, b.vpar, status)) return false;
-        tc_fence_after();
-        const uint32_t o = tmem + C::kO + (uint32_t)(w * D), pa = tmem + C::kP + (uint32_t)w * C::kPStep;
-        const uint64_t vd = vd0 + (uint64_t)((b.vi * C::kTile) >> 4);
-        umma_bf16_tmem_a_if(o, pa, vd, idesc_pv, b.first ? 0u : 1u, go);
-        if (b.slots == kSlots) {
-#pragma unroll
-          for (int s = 1; s < kSlots; ++s)
-            umma_bf16_tmem_a_if(o, pa + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv, 1u, go);
-        } else {
+      uint32_t half = 0;  // stages of V that one of their tile's two jobs has been finished with
+      bool end = false, need_q = false, need_k = false;  // what the tile in hand still waits for
+      int due = 0;                                       // the group that takes the next job
+      auto there = [&](uint64_t* bar, uint32_t par) { return __all_sync(0xffffffffu, mbar_test_wait(bar, par)) != 0; };
+      // The groups take jobs in turn; what is ready is issued, a group's product with V before its next scores.
+      // Nothing is waited for while something else could be issued: a tile's keys, its values, its queries' space and
+      // the groups' weights come in any order, and some only after what else is ready has been issued.
+      uint32_t idle = 0;
+      uint64_t since = 0;
 #pragma unroll 1
-          for (int s = 1; s < b.slots; ++s)
-            umma_bf16_tmem_a_if(o, pa + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv, 1u, go);
-        }
-        umma_commit_if(pv_done + w, go);
-        if (b.release) umma_commit_if(v_empty + b.vi, go);
-        ++b.done;
-        b.slots = 0;
-        return true;
-      };
-      // The groups take jobs in turn: group w's previous one is finished, then its next one begun, while the other
-      // group's scores are being worked on.
-      bool need_q = false;  // the tile in hand opens a unit whose queries have not been waited for
-      int due = 0;          // the group that takes the next job
+      while (true) {
+        bool progress = false;
 #pragma unroll 1
-      for (int w = 0; ok; w ^= 1) {
-        Job cur = w ? b : a;
-        if (cur.slots && !(ok = finish(cur, w))) break;
-        if (w)
-          b = cur;
-        else
-          a = cur;
-        const bool other = (w ? a : b).slots != 0;
-        if (w != due) continue;
-        while (left == 0 && !end && !need_q) {  // the next tile
-          if (!(ok = mbar_wait_ok(d_full + dr.i, dr.par, status))) break;
-          const TileDesc* td = descs + dr.i;
-          flags = td->flags;
-          slots = td->slots;
-          entry = td->entry;
-          if (flags & TD_END) {
-            end = true;
-            break;
-          }
-          mbar_arrive_lane0(d_empty + dr.i);
-          dr.next();
-          need_q = flags & TD_FIRST;
-          if (!need_q && slots) left = flags & TD_BOTH ? 2 : 1;
-        }
-        if (!ok) break;
-        if (end) {
-          if (!other) break;
-          continue;
-        }
-        if (need_q) {
-          // (the queries' space may wait for the unit of the other group's job: that is finished first)
-          const uint32_t par = (qpars >> entry) & 1u;
-          if (other && !__all_sync(0xffffffffu, mbar_test_wait(q_full + entry, par))) continue;
-          if (!(ok = mbar_wait_ok(q_full + entry, par, status))) break;
-          qpars ^= 1u << entry;
-          opened = 0;
-          need_q = false;
-          if (slots == 0) {
-            w ^= 1;  // (the same turn again)
-            continue;
-          }
-          left = flags & TD_BOTH ? 2 : 1;
-        }
-        due ^= 1;
-        if (new_tile && !(ok = mbar_wait_ok(k_full + kr.i, kr.par, status))) break;
-        new_tile = false;
-        // (without columns of its own, P lies where the next S goes)
-        if (!C::kOwnP && cur.done > 0 && !(ok = mbar_wait_ok(pv_done + w, (cur.done - 1) & 1u, status))) break;
-        tc_fence_after();
-        const uint64_t qd = qd0 + (uint64_t)(((flags & TD_BOTH ? w : entry) * C::kTile) >> 4);
-        const uint64_t kd = kd0 + (uint64_t)((kr.i * C::kTile) >> 4);
-        const uint32_t id = idesc | ((uint32_t)(slots * 2) << 17);
+        for (int e = 0; e < 2; ++e) {  // O += P V of a group's job, the older one first
+          const int w = due ^ e;
+          Job b_ = w ? b : a;
+          if (!b_.slots || !there(p_full + w, b_.done & 1u) || !there(v_ready + b_.vi, b_.vpar)) continue;
+          tc_fence_after();
+          const uint32_t o = tmem + C::kO + (uint32_t)(w * D), pa = tmem + C::kP + (uint32_t)w * C::kPStep;
+          const uint64_t vd = vd0 + (uint64_t)((b_.vi * C::kTile) >> 4);
+          umma_bf16_tmem_a_if(o, pa, vd, idesc_pv, b_.first ? 0u : 1u, go);
+          if (b_.slots == kSlots) {
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint64_t at = (uint64_t)(((kk * 32) / C::kRow * C::kHalf + (kk * 32) % C::kRow) >> 4);
-          umma_bf16_if(tmem + C::kS + (uint32_t)(w * 128), qd + at, kd + at, id, kk != 0 ? 1u : 0u, go);
+            for (int s = 1; s < kSlots; ++s)
+              umma_bf16_tmem_a_if(o, pa + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv, 1u, go);
+          } else {
+#pragma unroll 1
+            for (int s = 1; s < b_.slots; ++s)
+              umma_bf16_tmem_a_if(o, pa + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv, 1u, go);
+          }
+          umma_commit_if(pv_done + w, go);
+          // (two jobs of a tile, in either order: its values are free with the later one)
+          if (b_.shared) half ^= 1u << b_.vi;
+          if (!((half >> b_.vi) & 1u)) umma_commit_if(v_empty + b_.vi, go);
+          ++b_.done;
+          b_.slots = 0;
+          if (w)
+            b = b_;
+          else
+            a = b_;
+          progress = true;
         }
-        umma_commit_if(s_full + w, go);
-        --left;
-        if (left == 0) umma_commit_if(k_empty + kr.i, go);
-        cur = Job{slots, (opened >> w) & 1 ? 0 : 1, left == 0, vr.i, vr.par, cur.done};
-        opened |= 1 << w;
-        if (w)
-          b = cur;
-        else
-          a = cur;
-        if (left == 0) {
-          kr.next();
-          vr.next();
-          new_tile = true;
+        Job cur = due ? b : a;
+        if (!cur.slots && !end) {
+          if (left == 0 && !need_q && there(d_full + dr.i, dr.par)) {
+            const TileDesc* td = descs + dr.i;
+            flags = td->flags;
+            slots = td->slots;
+            entry = td->entry;
+            progress = true;
+            if (flags & TD_END) {
+              end = true;
+            } else {
+              mbar_arrive_lane0(d_empty + dr.i);
+              dr.next();
+              need_q = flags & TD_FIRST;
+              need_k = true;
+              left = slots == 0 ? 0 : flags & TD_BOTH ? 2 : 1;
+            }
+          }
+          if (need_q && there(q_full + entry, (qpars >> entry) & 1u)) {
+            qpars ^= 1u << entry;
+            opened = 0;
+            need_q = false;
+            progress = true;
+          }
+          if (need_k && left && there(k_full + kr.i, kr.par)) need_k = false;
+          // (without columns of its own, P lies where the next S goes)
+          if (left && !need_q && !need_k && (C::kOwnP || cur.done == 0 || there(pv_done + due, (cur.done - 1) & 1u))) {
+            tc_fence_after();
+            const int w = due;
+            const uint64_t qd = qd0 + (uint64_t)(((flags & TD_BOTH ? w : entry) * C::kTile) >> 4);
+            const uint64_t kd = kd0 + (uint64_t)((kr.i * C::kTile) >> 4);
+            const uint32_t id = idesc | ((uint32_t)(slots * 2) << 17);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+              const uint64_t at = (uint64_t)(((kk * 32) / C::kRow * C::kHalf + (kk * 32) % C::kRow) >> 4);
+              umma_bf16_if(tmem + C::kS + (uint32_t)(w * 128), qd + at, kd + at, id, kk != 0 ? 1u : 0u, go);
+            }
+            umma_commit_if(s_full + w, go);
+            --left;
+            if (left == 0) umma_commit_if(k_empty + kr.i, go);
+            cur = Job{slots, (opened >> w) & 1 ? 0 : 1, flags & TD_BOTH ? 1 : 0, vr.i, vr.par, cur.done};
+            opened |= 1 << w;
+            if (w)
+              b = cur;
+            else
+              a = cur;
+            if (left == 0) {
+              kr.next();
+              vr.next();
+            }
+            due ^= 1;
+            progress = true;
+          }
+        }
+        if (end && !a.slots && !b.slots) break;
+        // bounded, as every wait
+        if (progress) {
+          idle = 0;
+        } else if ((++idle & 255u) == 0) {
+          const uint64_t now = globaltimer_ns();
+          if (idle == 256) since = now;
+          bool stop = now - since > (uint64_t)kWaitLimitUs * 1000u;
+          if (stop) atomicOr(status, ST_TIMEOUT);
+          stop = stop || (*reinterpret_cast<volatile int*>(status) & ST_TIMEOUT);
+          if (__any_sync(0xffffffffu, stop)) break;
         }
       }
       umma_drain(drain, status, go);
@@ -1300,11 +1319,11 @@ const Device& device() {
   return devs[d];
 }
 
-// [n_pages * kv_heads * page_rows, head_dim] in boxes of 16 rows by 128 (or 64) bytes
-bool encode_pages(CUtensorMap* m, const fe_paged_kv& kv, const void* base) {
+// [n_pages * kv_heads * page_rows, head_dim] in boxes of some rows by 128 (or 64) bytes
+bool encode_pages(CUtensorMap* m, const fe_paged_kv& kv, const void* base, int rows) {
   const cuuint64_t dims[2] = {(cuuint64_t)kv.head_dim, (cuuint64_t)kv.n_pages * kv.kv_heads * kv.page_rows};
   const cuuint64_t strides[1] = {(cuuint64_t)kv.head_dim * 2};
-  const cuuint32_t box[2] = {(cuuint32_t)(kv.head_dim < 64 ? kv.head_dim : 64), (cuuint32_t)kSlot}, es[2] = {1u, 1u};
+  const cuuint32_t box[2] = {(cuuint32_t)(kv.head_dim < 64 ? kv.head_dim : 64), (cuuint32_t)rows}, es[2] = {1u, 1u};
   const EncodeTiledFn fn = encode_tiled_fn();
   return fn && fn(m, kv.dtype == FE_IO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
                   const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -1313,17 +1332,17 @@ bool encode_pages(CUtensorMap* m, const fe_paged_kv& kv, const void* base) {
 }
 
 template <typename T, int D>
-cudaError_t prefix_go(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, cudaStream_t s) {
+cudaError_t prefix_go(const PageMaps& m, const PrefixParams& p, cudaStream_t s) {
   using C = PrefixCfg<D>;
   cudaError_t e = launch_k(prefix_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
   if (e == cudaSuccess)
-    e = launch_k(prefix_attend_kernel<T, D>, dim3((unsigned)p.ctas), dim3(C::kThreads), C::kSmem, s, tk, tv, p);
+    e = launch_k(prefix_attend_kernel<T, D>, dim3((unsigned)p.ctas), dim3(C::kThreads), C::kSmem, s, m, p);
   if (e == cudaSuccess) e = launch_k(prefix_finish_kernel<T, D>, dim3((unsigned)p.ctas, 8), dim3(256), 0, s, p);
   return e;
 }
 template <typename T>
-cudaError_t prefix_dim(const CUtensorMap& tk, const CUtensorMap& tv, const PrefixParams& p, int d, cudaStream_t s) {
-  return d == 32 ? prefix_go<T, 32>(tk, tv, p, s) : d == 64 ? prefix_go<T, 64>(tk, tv, p, s) : prefix_go<T, 128>(tk, tv, p, s);
+cudaError_t prefix_dim(const PageMaps& m, const PrefixParams& p, int d, cudaStream_t s) {
+  return d == 32 ? prefix_go<T, 32>(m, p, s) : d == 64 ? prefix_go<T, 64>(m, p, s) : prefix_go<T, 128>(m, p, s);
 }
 
 }  // namespace
@@ -1386,14 +1405,16 @@ extern "C" int fe_prefix_attention(const fe_prefix_args* a, void* stream) {
   p.prefix_cols = a->prefix_cols;
   p.page_cols = a->page_cols;
   p.page_rows = a->kv.page_rows;
+  while ((1 << p.page_shift) < p.page_rows) ++p.page_shift;
   p.n_pages = a->kv.n_pages;
   p.scale = a->scale;
   p.sc = std::fmax((float)(a->scale * 1.4426950408889634), 1e-30f);
-  CUtensorMap tk, tv;
-  if (!encode_pages(&tk, a->kv, a->kv.k) || !encode_pages(&tv, a->kv, a->kv.v))
+  PageMaps m;
+  if (!encode_pages(&m.k, a->kv, a->kv.k, kSlot) || !encode_pages(&m.v, a->kv, a->kv.v, kSlot) ||
+      !encode_pages(&m.k_page, a->kv, a->kv.k, p.page_rows) || !encode_pages(&m.v_page, a->kv, a->kv.v, p.page_rows))
     return fail(FE_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = a->kv.dtype == FE_IO_BF16 ? prefix_dim<__nv_bfloat16>(tk, tv, p, a->kv.head_dim, s)
-                                                  : prefix_dim<__half>(tk, tv, p, a->kv.head_dim, s);
+  const cudaError_t e = a->kv.dtype == FE_IO_BF16 ? prefix_dim<__nv_bfloat16>(m, p, a->kv.head_dim, s)
+                                                  : prefix_dim<__half>(m, p, a->kv.head_dim, s);
   return e == cudaSuccess ? FE_OK : fail_cuda(e, "fe_prefix_attention");
 }
