@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kPlanThreads) prefix_plan_kernel(const PrefixP
 // attend
 // ---------------------------------------------------------------------------
 // What the loading warp tells the others about a key tile
-struct TileDesc {
+struct alignas(16) TileDesc {
   int flags, slots, bad, clean, piece, entry, pad[2];
   int owner[kSlots];  // sequence, or -1: the prefix
   int base[kSlots];   // the slot's first key
@@ -373,8 +373,11 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       const long long total = bad_plan ? 0 : p.gcost[p.n_groups];
       // (no more CTAs than tiles: each of them has one at least)
       const int ctas = (int)min((long long)p.ctas, total);
-      const long long hi = cta < ctas ? total * (cta + 1) / ctas : 0;
-      long long x = cta < ctas ? total * cta / ctas : 0;
+      const long long each = ctas > 0 ? total / ctas : 0;
+      const int more = (int)(total - each * ctas);  // CTAs with one tile more
+      auto begin = [&](int c) { return each * c + min(c, more); };
+      const long long hi = cta < ctas ? begin(cta + 1) : 0;
+      long long x = cta < ctas ? begin(cta) : 0;
       Ring<NK> kr;
       Ring<NV> vr;
       Ring<ND> dr;
@@ -396,9 +399,10 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         // (groups without rows have no tiles: the last of equal starts is the one with some)
         g = find_last(p.gcost, p.n_groups + 1, x);
         open_group();
-        const long long per_head = (p.gcost[g + 1] - p.gcost[g]) / p.hkv, rem = x - p.gcost[g];
-        head = (int)(rem / per_head);
-        const long long y = rem - (long long)head * per_head + p.before[first_rt];
+        const long long per_head = p.before[first_rt + n_rt] - p.before[first_rt];
+        long long y = x - p.gcost[g];
+        while (y >= per_head) y -= per_head, ++head;
+        y += p.before[first_rt];
         ti = find_last(p.before + first_rt, n_rt, y);
         off = (int)(y - p.before[first_rt + ti]);
       }
@@ -412,7 +416,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           const long long end = x + cost;
           int c = cta + 1;
 #pragma unroll 1
-          while (c < ctas && total * c / ctas < end) ++c;
+          while (c < ctas && begin(c) < end) ++c;
           rec = SplitRec{c - cta - 1, t0, r0, rows, head, {}};
         }
         // tell the query loader
@@ -728,24 +732,33 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         if (slots > 0) {
           if (!mbar_wait_ok(v_full + vr.i, vr.par, status)) break;
           uint8_t* v = sV + vr.i * C::kTile;
-          if (flags & TD_SCAN) {
-            // one pass: rows past a slot's end cleared, the others' 0 x summed: 0 as long as every x is a number
-            uint32_t acc = 0;
 #pragma unroll 1
-            for (int hf = 0; hf < C::NH; ++hf)
-#pragma unroll 2
-              for (uint32_t o = lane * 16; o < (uint32_t)slots * kSlot * C::kRow; o += 512) {
-                const uint32_t r = o / C::kRow;
-                uint4* x = reinterpret_cast<uint4*>(v + hf * C::kHalf + o);
-                if ((int)(r % kSlot) >= __shfl_sync(0xffffffffu, count, r / kSlot)) {
-                  *x = make_uint4(0u, 0u, 0u, 0u);
-                } else {
-                  const uint4 y = *x;
-                  acc = Elem<T>::zero_fma(y.x, Elem<T>::zero_fma(y.y, Elem<T>::zero_fma(y.z, Elem<T>::zero_fma(y.w, acc))));
-                }
-              }
+          for (uint32_t left = (uint32_t)clean; left; left &= left - 1) {  // rows past a slot's end (whole rows: the
+            const int sl = __ffs(left) - 1, n = __shfl_sync(0xffffffffu, count, sl);  // swizzle moves pieces in a row)
+#pragma unroll
+            for (int o = 0; o < (int)(C::NH * kSlot * C::kRow); o += 512) {
+              const int in = (o % (int)(kSlot * C::kRow)) + lane * 16;
+              if (in >= n * (int)C::kRow)
+                *reinterpret_cast<uint4*>(v + o / (int)(kSlot * C::kRow) * C::kHalf + sl * kSlot * C::kRow + in) =
+                    make_uint4(0u, 0u, 0u, 0u);
+            }
+          }
+          if (flags & TD_SCAN) {
             __syncwarp();
-            if (__any_sync(0xffffffffu, (acc & 0x7fff7fffu) != 0)) {
+            // 0 x summed: 0 as long as every x is a number
+            uint32_t acc[4] = {0u, 0u, 0u, 0u};
+#pragma unroll 1
+            for (int sl = 0; sl < slots; ++sl)
+#pragma unroll
+              for (int o = 0; o < (int)(C::NH * kSlot * C::kRow); o += 512) {
+                const uint4 y = *reinterpret_cast<const uint4*>(v + o / (int)(kSlot * C::kRow) * C::kHalf + sl * kSlot * C::kRow +
+                                                                o % (int)(kSlot * C::kRow) + lane * 16);
+                acc[0] = Elem<T>::zero_fma(y.x, acc[0]);
+                acc[1] = Elem<T>::zero_fma(y.y, acc[1]);
+                acc[2] = Elem<T>::zero_fma(y.z, acc[2]);
+                acc[3] = Elem<T>::zero_fma(y.w, acc[3]);
+              }
+            if (__any_sync(0xffffffffu, ((acc[0] | acc[1] | acc[2] | acc[3]) & 0x7fff7fffu) != 0)) {
 #pragma unroll 1
               for (int s = 0; s < slots; ++s) {
                 bool found = false;
@@ -770,15 +783,6 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
                   }
                 }
               }
-            }
-          } else if (clean) {
-#pragma unroll 1
-            for (uint32_t left = (uint32_t)clean; left; left &= left - 1) {
-              const int s = __ffs(left) - 1, n = __shfl_sync(0xffffffffu, count, s);
-              // (whole rows: the swizzle moves pieces within a row)
-              for (int hf = 0; hf < C::NH; ++hf)
-                for (uint32_t o = (uint32_t)n * C::kRow + lane * 16; o < kSlot * C::kRow; o += 512)
-                  *reinterpret_cast<uint4*>(v + hf * C::kHalf + s * kSlot * C::kRow + o) = make_uint4(0u, 0u, 0u, 0u);
             }
           }
           fence_async_shared();
@@ -894,6 +898,9 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           float mx = -INFINITY;
           uint32_t pairs = 0, seen0 = 0, seen1 = 0;  // pairs with a key that a row of the warp sees; this row's keys of
                                                      // slots 0 .. 3 and 4 .. 7, a byte each
+          bool single = false;
+          int slot = -1;
+          float one[kSlot];
           auto pair = [&](int z, float* v) {  // scores of slots 2 z and 2 z + 1, unseen ones -inf
             tmem_ld32(t_s + (uint32_t)(32 * z), v);
             const uint32_t two = (z < 2 ? seen0 : seen1) >> (16 * (z & 1));
@@ -912,22 +919,55 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
               mx = fmaxf(mx, maxn<64>(v));
             }
           } else {
-            const int bad = td->bad;
+            // this row's keys of a slot: of the prefix all valid ones, of its own sequence those up to itself
+            const int4 *own4 = reinterpret_cast<const int4*>(td->owner), *base4 = reinterpret_cast<const int4*>(td->base),
+                       *count4 = reinterpret_cast<const int4*>(td->count);
+            uint32_t mask = 0;
 #pragma unroll
-            for (int at = 0; at < kSlots; ++at) {
-              const int owner = td->owner[at], count = td->count[at];
-              int n = owner == -1 ? count : owner == ri.seq ? min(count, max(0, ri.seen - td->base[at])) : 0;
-              if (at >= slots) n = 0;
-              spoiled = spoiled || (n > 0 && ((bad >> at) & 1));
-              (at < 4 ? seen0 : seen1) |= (uint32_t)n << (8 * (at & 3));
+            for (int h = 0; h < 2; ++h) {
+              const int4 ow = own4[h], ba = base4[h], co = count4[h];
+              auto n_of = [&](int owner, int base, int count) {
+                const int most = owner == -1 ? 1 << 30 : owner == ri.seq ? ri.seen : -(1 << 30);
+                return (uint32_t)min(count, max(0, most - base));
+              };
+              const uint32_t n0 = n_of(ow.x, ba.x, co.x), n1 = n_of(ow.y, ba.y, co.y), n2 = n_of(ow.z, ba.z, co.z),
+                             n3 = n_of(ow.w, ba.w, co.w);
+              (h ? seen1 : seen0) = n0 | n1 << 8 | n2 << 16 | n3 << 24;
+              mask |= ((n0 ? 1u : 0u) | (n1 ? 2u : 0u) | (n2 ? 4u : 0u) | (n3 ? 8u : 0u)) << (4 * h);
             }
-            pairs = (__any_sync(0xffffffffu, seen0 & 0xffffu) ? 1u : 0u) | (__any_sync(0xffffffffu, seen0 >> 16) ? 2u : 0u) |
-                    (__any_sync(0xffffffffu, seen1 & 0xffffu) ? 4u : 0u) | (__any_sync(0xffffffffu, seen1 >> 16) ? 8u : 0u);
+            spoiled = spoiled || (mask & (uint32_t)td->bad);
+            const uint32_t any = __reduce_or_sync(0xffffffffu, mask);
+            pairs = (any & 3u ? 1u : 0u) | (any & 12u ? 2u : 0u) | (any & 48u ? 4u : 0u) | (any & 192u ? 8u : 0u);
+            single = __all_sync(0xffffffffu, __popc(mask) <= 1);
+            if (single) {
+              // every row of the warp sees one slot at most (short sequences): 16 scores each, picked from the pairs
+              slot = __ffs(mask) - 1;
+              const int n = slot < 0 ? 0 : (int)(((slot < 4 ? seen0 : seen1) >> (8 * (slot & 3))) & 0xffu);
+#pragma unroll
+              for (int i = 0; i < kSlot; ++i) one[i] = -INFINITY;
+#pragma unroll 1
+              for (uint32_t left = pairs; left; left &= left - 1) {
+                const int z = __ffs(left) - 1;
+                float v[32];
+                tmem_ld32(t_s + (uint32_t)(32 * z), v);
+#pragma unroll
+                for (int i = 0; i < kSlot; ++i) {
+                  if (slot == 2 * z) one[i] = v[i];
+                  if (slot == 2 * z + 1) one[i] = v[kSlot + i];
+                }
+              }
+#pragma unroll
+              for (int i = 0; i < kSlot; ++i) {
+                if (i >= n) one[i] = -INFINITY;
+              }
+              mx = maxn<kSlot>(one);
+            } else {
 #pragma unroll 1
             for (uint32_t left = pairs; left; left &= left - 1) {
               float v[32];
               pair(__ffs(left) - 1, v);
               mx = fmaxf(mx, maxn<32>(v));
+            }
             }
           }
           mx *= sc;
@@ -960,10 +1000,9 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           const float ref = m == -INFINITY ? 0.f : m;
           const uint64_t sc2 = f32x2_pack(sc, sc), nm2 = f32x2_pack(-ref, -ref);
           uint64_t sum[2] = {0ull, 0ull};
-          auto weights = [&](const float* x, int c0) {  // P of 32 keys from column c0 of S on
-            uint32_t pk[16];
+          auto weights = [&](const float* x, auto count, uint32_t* pk) {  // P of some keys, in pairs
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
+            for (int i = 0; i < decltype(count)::value; i += 4) {
               float e[4];
               f32x2_unpack(f32x2_fma(f32x2_pack(x[i], x[i + 1]), sc2, nm2), e[0], e[1]);
               f32x2_unpack(f32x2_fma(f32x2_pack(x[i + 2], x[i + 3]), sc2, nm2), e[2], e[3]);
@@ -974,23 +1013,42 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
               pk[i / 2] = Elem<T>::put2(e[0], e[1]);
               pk[i / 2 + 1] = Elem<T>::put2(e[2], e[3]);
             }
-            tmem_st16_nowait(t_p + (uint32_t)(c0 / 2), pk);
           };
+          const std::integral_constant<int, 32> c32{};
           if (whole) {
 #pragma unroll 1
             for (int c0 = 0; c0 < 128; c0 += 64) {
               float v[64];
               tmem_ld64(t_s + (uint32_t)c0, v);
-              weights(v, c0);
-              weights(v + 32, c0 + 32);
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                uint32_t pk[16];
+                weights(v + 32 * h, c32, pk);
+                tmem_st16_nowait(t_p + (uint32_t)(c0 / 2 + 16 * h), pk);
+              }
+            }
+          } else if (single) {
+            uint32_t mine8[kSlot / 2];
+            weights(one, std::integral_constant<int, kSlot>(), mine8);
+#pragma unroll 1
+            for (int z = 0; 2 * z < slots; ++z) {
+              uint32_t pk[16];
+#pragma unroll
+              for (int i = 0; i < kSlot / 2; ++i) {
+                pk[i] = slot == 2 * z ? mine8[i] : 0u;
+                pk[kSlot / 2 + i] = slot == 2 * z + 1 ? mine8[i] : 0u;
+              }
+              tmem_st16_nowait(t_p + (uint32_t)(16 * z), pk);
             }
           } else {
 #pragma unroll 1
             for (int z = 0; 2 * z < slots; ++z) {
               if ((pairs >> z) & 1) {
                 float v[32];
+                uint32_t pk[16];
                 pair(z, v);
-                weights(v, 32 * z);
+                weights(v, c32, pk);
+                tmem_st16_nowait(t_p + (uint32_t)(16 * z), pk);
               } else {
                 const uint32_t zero[16] = {};
                 tmem_st16_nowait(t_p + (uint32_t)(16 * z), zero);
