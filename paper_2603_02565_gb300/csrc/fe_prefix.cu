@@ -225,10 +225,11 @@ __global__ void __launch_bounds__(kPlanThreads) prefix_plan_kernel(const PrefixP
 // ---------------------------------------------------------------------------
 // What the loading warp tells the others about a key tile
 struct alignas(16) TileDesc {
-  int flags, slots, bad, clean, piece, entry, pad[2];
+  int flags, slots, bad, piece, entry, pad[3];
   int owner[kSlots];  // sequence, or -1: the prefix
   int base[kSlots];   // the slot's first key
   int count[kSlots];  // its valid keys
+  int row[kSlots];    // the first one's row of the pages
 };
 enum : int { TD_FIRST = 1, TD_LAST = 2, TD_BOTH = 4, TD_FULL = 8, TD_END = 16, TD_SCAN = 32 };
 struct UnitInfo {
@@ -243,9 +244,9 @@ struct Dirty {
   int n, seq[kDirty];  // n > kDirty: any of them
 };
 
-// Tensor maps of the pages: a slot of 16 rows, and the page or tile, whichever is smaller
+// Tensor maps of the pages, a page a box
 struct PageMaps {
-  CUtensorMap k, v, k_page, v_page;
+  CUtensorMap k, v;
 };
 
 template <int D>
@@ -283,6 +284,60 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait_group() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+// 16 bytes, or 16 zeros
+__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ bool there(uint64_t* bar, uint32_t par) {  // for the whole warp
+  return __all_sync(0xffffffffu, mbar_test_wait(bar, par)) != 0;
+}
+
+// A whole tile: eight full slots of a prefix, whose pages follow one another in the tile: a box a page and half.
+template <int D>
+__device__ __forceinline__ void load_pages(uint8_t* dst, const CUtensorMap* map, uint64_t* bar, int row, int lane0, int page_rows,
+                                           uint32_t go) {
+  using C = PrefixCfg<D>;
+  mbar_arrive_expect_tx_if(bar, C::kTile, go);
+#pragma unroll 1
+  for (int i = 0; i < kSlots; i += page_rows / kSlot) {
+    const int r = __shfl_sync(0xffffffffu, row, lane0 + i);
+#pragma unroll
+    for (int hf = 0; hf < C::NH; ++hf)
+      tma_load_2d_if(dst + hf * C::kHalf + i * kSlot * C::kRow, map, 64 * hf, r, bar, go);
+  }
+}
+// Any other tile: slot by slot, its valid rows alone, the others zeros (ZERO) or left as they are.  Boxes cost about
+// 100 cycles each to issue whatever their size (16 of them 1900 of a tile's cycles); this takes a few hundred, and
+// reads no row that is not used.
+template <int D, bool ZERO>
+__device__ __forceinline__ void load_slots(uint8_t* dst, const void* pages, int slots, int row, int count, int lane0) {
+  using C = PrefixCfg<D>;
+  constexpr int NP = D / 8, RP = 32 / NP;  // pieces of a row, rows of a step
+  const int lane = threadIdx.x & 31, r0 = lane / NP, pc = lane % NP;
+  const uint32_t at = smem_u32(dst) + (uint32_t)(pc * 16) / C::kRow * C::kHalf + (uint32_t)r0 * C::kRow;
+  const uint32_t poff = (uint32_t)(pc * 16) % C::kRow;
+  const char* src = static_cast<const char*>(pages) + (r0 * D + pc * 8) * 2;
+#pragma unroll 1
+  for (int s = 0; s < slots; ++s) {
+    const int r = __shfl_sync(0xffffffffu, row, lane0 + s), n = __shfl_sync(0xffffffffu, count, lane0 + s);
+    const char* from = src + (long long)r * (D * 2);
+#pragma unroll
+    for (int i = 0; i < kSlot; i += RP) {
+      const uint32_t in = (uint32_t)(r0 + i);  // row of the slot (a slot begins a swizzle pattern)
+      const uint32_t mask = C::kRow == 128 ? (in & 7u) : ((in >> 1) & 3u);
+      const uint32_t to = at + (uint32_t)(s * kSlot + i) * C::kRow + (poff ^ (mask << 4));
+      if (ZERO)
+        cp_async16_or_zero(to, from + (r0 + i < n ? i * D * 2 : -(r0 * D * 2)), r0 + i < n);
+      else if (r0 + i < n)
+        cp_async16(to, from + i * D * 2);
+    }
+  }
+}
 __device__ __forceinline__ void mbar_arrive_lane0(uint64_t* bar) {
   __syncwarp();
   mbar_arrive_if_at(smem_u32(bar), (threadIdx.x & 31) == 0);
@@ -352,8 +407,6 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
     fence_mbar_init();
     prefetch_tmap(&maps.k);
     prefetch_tmap(&maps.v);
-    prefetch_tmap(&maps.k_page);
-    prefetch_tmap(&maps.v_page);
   }
   if (warp == 1) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
@@ -366,7 +419,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
 
   if (warp < 4) {
     if (warp == 0) {
-      // ---------------- schedule and loads ----------------
+      // ---------------- schedule and keys ----------------
       const int cta = blockIdx.x;
       const uint32_t go = elect_one();
       const bool bad_plan = p.head->bad != 0;
@@ -379,11 +432,29 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       const long long hi = cta < ctas ? begin(cta + 1) : 0;
       long long x = cta < ctas ? begin(cta) : 0;
       Ring<NK> kr;
-      Ring<NV> vr;
       Ring<ND> dr;
       Ring<2> ur;
       bool ok = true;
       SplitRec rec = {};
+      // Slots on their way by cp.async, oldest first: their tiles are announced once they have landed, at the latest
+      // before this warp waits for anything.
+      int away = 0;
+      uint64_t *away0 = nullptr, *away1 = nullptr;
+      auto landed = [&](bool all) {
+        if (all)
+          cp_async_wait_group<0>();
+        else
+          cp_async_wait_group<2>();
+        fence_async_shared();
+        mbar_arrive_lane0(away0);
+        if (all && away == 2) mbar_arrive_lane0(away1);
+        away0 = away1;
+        away = all ? 0 : away - 1;
+      };
+      auto wait = [&](uint64_t* bar, uint32_t par) {
+        if (away && !there(bar, par)) landed(true);
+        return mbar_wait_ok(bar, par, status);
+      };
       // the unit that holds tile x: group, head, row tile; the next ones follow step by step
       int g = 0, head = 0, ti = 0, off = 0, first_rt = 0, n_rt = 0, s0 = 0, s1 = 0, t0 = 0, group_rows = 0, plen = 0;
       auto open_group = [&]() {
@@ -420,7 +491,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           rec = SplitRec{c - cta - 1, t0, r0, rows, head, {}};
         }
         // tell the query loader
-        if (!(ok = mbar_wait_ok(u_empty + ur.i, ur.par ^ 1u, status))) break;
+        if (!(ok = wait(u_empty + ur.i, ur.par ^ 1u))) break;
         if (lane == 0) units[ur.i] = UnitInfo{t0, r0, rows, head, both, g, 0, 0};
         mbar_arrive_lane0(u_full + ur.i);
         const int entry = ur.i;
@@ -517,45 +588,39 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           const uint32_t used = __ballot_sync(0xffffffffu, mine && b_owner != -2);
           const uint32_t badm = __ballot_sync(0xffffffffu, mine && b_bad), part_m = __ballot_sync(0xffffffffu, mine && b_owner != -2 && b_count < kSlot);
           const int slots = __popc(used);
-          if (!(ok = mbar_wait_ok(d_empty + dr.i, dr.par ^ 1u, status))) break;
+          const bool whole = part == 0 && slots == kSlots && part_m == 0 && badm == 0;
+          if (!(ok = wait(d_empty + dr.i, dr.par ^ 1u))) break;
           TileDesc* td = descs + dr.i;
           if (mine) {
             td->owner[lane - l0] = b_owner;
             td->base[lane - l0] = b_base;
             td->count[lane - l0] = b_count;
+            td->row[lane - l0] = b_row;
           }
           if (lane == 0) {
             td->flags = (j == off ? TD_FIRST : 0) | (j == off + n - 1 ? TD_LAST : 0) | (both ? TD_BOTH : 0) |
-                        (part == 0 && slots == kSlots && part_m == 0 && badm == 0 ? TD_FULL : 0) |
+                        (whole ? TD_FULL : 0) |
                         (part == 1 && ta != tb ? TD_SCAN : 0);
             td->slots = slots;
             td->bad = (int)(badm >> l0);
-            td->clean = (int)(part_m >> l0);
             td->piece = piece;
             td->entry = entry;
           }
           mbar_arrive_lane0(d_full + dr.i);
           dr.next();
           if (slots == 0) continue;
-          const uint32_t bytes = (uint32_t)slots * kSlot * D * 2;
-          const bool whole = slots == kSlots && part == 0 && part_m == 0 && badm == 0;  // pages follow one another
-          const int step = whole ? p.page_rows / kSlot : 1;
-          auto load = [&](uint8_t* dst, const CUtensorMap* map, uint64_t* bar) {
-            mbar_arrive_expect_tx_if(bar, bytes, go);
-#pragma unroll 1
-            for (int i = 0; i < slots; i += step) {
-              const int r = __shfl_sync(0xffffffffu, b_row, l0 + i);
-#pragma unroll
-              for (int hf = 0; hf < C::NH; ++hf)
-                tma_load_2d_if(dst + hf * C::kHalf + i * kSlot * C::kRow, map, 64 * hf, r, bar, go);
-            }
-          };
-          if (!(ok = mbar_wait_ok(k_empty + kr.i, kr.par ^ 1u, status))) break;
-          load(sK + kr.i * C::kTile, whole ? &maps.k_page : &maps.k, k_full + kr.i);
+          if (!(ok = wait(k_empty + kr.i, kr.par ^ 1u))) break;
+          if (whole) {
+            load_pages<D>(sK + kr.i * C::kTile, &maps.k, k_full + kr.i, b_row, l0, p.page_rows, go);
+            cp_async_commit();
+          } else {
+            load_slots<D, false>(sK + kr.i * C::kTile, p.k, slots, b_row, b_count, l0);
+            cp_async_commit();
+            if (away == 2) landed(false);
+            (away ? away1 : away0) = k_full + kr.i;
+            ++away;
+          }
           kr.next();
-          if (!(ok = mbar_wait_ok(v_empty + vr.i, vr.par ^ 1u, status))) break;
-          load(sV + vr.i * C::kTile, whole ? &maps.v_page : &maps.v, v_full + vr.i);
-          vr.next();
         }
         // the next unit: row tile, head, group with rows
         off = 0;
@@ -570,6 +635,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           }
         }
       }
+      if (away) landed(true);
       if (ok && mbar_wait_ok(d_empty + dr.i, dr.par ^ 1u, status)) {
         if (lane == 0) descs[dr.i].flags = TD_END;
         mbar_arrive_lane0(d_full + dr.i);
@@ -581,7 +647,6 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       if (lane == 0) p.recs[cta] = rec;
       // the loads land before the shared memory goes away, whatever became of their readers
       mbar_landed_ring(k_full, kr.i, kr.par ^ 1u, NK, status);
-      mbar_landed_ring(v_full, vr.i, vr.par ^ 1u, NV, status);
     } else if (warp == 1) {
       // ---------------- products ----------------
       const uint32_t go = elect_one();
@@ -607,7 +672,6 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       uint32_t half = 0;  // stages of V that one of their tile's two jobs has been finished with
       bool end = false, need_q = false, need_k = false;  // what the tile in hand still waits for
       int due = 0;                                       // the group that takes the next job
-      auto there = [&](uint64_t* bar, uint32_t par) { return __all_sync(0xffffffffu, mbar_test_wait(bar, par)) != 0; };
       // The groups take jobs in turn; what is ready is issued, a group's product with V before its next scores.
       // Nothing is waited for while something else could be issued: a tile's keys, its values, its queries' space and
       // the groups' weights come in any order, and some only after what else is ready has been issued.
@@ -716,39 +780,69 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       umma_drain(drain, status, go);
     } else if (warp == 2) {
       // ---------------- values ----------------
+      // A tile is loaded, and the one before it then made ready (or at once, while the next has to wait).
+      const uint32_t go = elect_one();
       Ring<NV> vr;
       Ring<ND> dr;
-      uint32_t unit = 0;
-      while (true) {
-        if (!mbar_wait_ok(d_full + dr.i, dr.par, status)) break;
-        const TileDesc* td = descs + dr.i;
-        const int flags = td->flags, slots = td->slots, clean = td->clean;
-        const int count = lane < kSlots ? td->count[lane] : 0, owner = lane < kSlots ? td->owner[lane] : -1;
-        if (flags & TD_END) break;
-        mbar_arrive_lane0(d_empty + dr.i);
-        dr.next();
-        Dirty* dt = dirty + unit % kUnitsAhead;
-        if ((flags & TD_FIRST) && lane == 0) dt->n = 0;
-        if (slots > 0) {
-          if (!mbar_wait_ok(v_full + vr.i, vr.par, status)) break;
-          uint8_t* v = sV + vr.i * C::kTile;
+      uint32_t unit = 0, full = 0;  // unit: of the tile to be made ready; parities of the stages' box loads
+      struct Tile {
+        int flags, slots, stage, owner, row, count;  // (owner, row and count: of this lane's slot)
+      };
+      Tile next = {}, last = {};
+      bool have = false, pending = false, issued = false, end = false, ok = true;
 #pragma unroll 1
-          for (uint32_t left = (uint32_t)clean; left; left &= left - 1) {  // rows past a slot's end (whole rows: the
-            const int sl = __ffs(left) - 1, n = __shfl_sync(0xffffffffu, count, sl);  // swizzle moves pieces in a row)
-#pragma unroll
-            for (int o = 0; o < (int)(C::NH * kSlot * C::kRow); o += 512) {
-              const int in = (o % (int)(kSlot * C::kRow)) + lane * 16;
-              if (in >= n * (int)C::kRow)
-                *reinterpret_cast<uint4*>(v + o / (int)(kSlot * C::kRow) * C::kHalf + sl * kSlot * C::kRow + in) =
-                    make_uint4(0u, 0u, 0u, 0u);
-            }
+      while (true) {
+        issued = false;
+        if (!have && !end && (!pending || there(d_full + dr.i, dr.par))) {
+          if (!(ok = mbar_wait_ok(d_full + dr.i, dr.par, status))) break;
+          const TileDesc* td = descs + dr.i;
+          next.flags = td->flags;
+          next.slots = td->slots;
+          next.owner = td->owner[lane & (kSlots - 1)];
+          next.row = td->row[lane & (kSlots - 1)];
+          next.count = td->count[lane & (kSlots - 1)];
+          if (next.flags & TD_END) {
+            end = true;
+          } else {
+            mbar_arrive_lane0(d_empty + dr.i);
+            dr.next();
+            have = true;
           }
-          if (flags & TD_SCAN) {
+        }
+        if (have && (!pending || next.slots == 0 || there(v_empty + vr.i, vr.par ^ 1u))) {
+          next.stage = vr.i;
+          if (next.slots > 0) {
+            if (!(ok = mbar_wait_ok(v_empty + vr.i, vr.par ^ 1u, status))) break;
+            uint8_t* v = sV + vr.i * C::kTile;
+            if (next.flags & TD_FULL)
+              load_pages<D>(v, &maps.v, v_full + vr.i, next.row, 0, p.page_rows, go);
+            else
+              load_slots<D, true>(v, p.v, next.slots, next.row, next.count, 0);
+            vr.next();
+          }
+          cp_async_commit();
+          have = false;
+          issued = true;
+        }
+        if (pending) {
+          const uint32_t bit = 1u << last.stage;
+          Dirty* dt = dirty + unit % kUnitsAhead;
+          if ((last.flags & TD_FIRST) && lane == 0) dt->n = 0;
+          if (last.flags & TD_FULL) {
+            if (!(ok = mbar_wait_ok(v_full + last.stage, (full & bit) ? 1u : 0u, status))) break;
+            full ^= bit;
+          } else if (issued) {
+            cp_async_wait_group<1>();
+          } else {
+            cp_async_wait_group<0>();
+          }
+          if (last.flags & TD_SCAN) {
             __syncwarp();
+            uint8_t* v = sV + last.stage * C::kTile;
             // 0 x summed: 0 as long as every x is a number
             uint32_t acc[4] = {0u, 0u, 0u, 0u};
 #pragma unroll 1
-            for (int sl = 0; sl < slots; ++sl)
+            for (int sl = 0; sl < last.slots; ++sl)
 #pragma unroll
               for (int o = 0; o < (int)(C::NH * kSlot * C::kRow); o += 512) {
                 const uint4 y = *reinterpret_cast<const uint4*>(v + o / (int)(kSlot * C::kRow) * C::kHalf + sl * kSlot * C::kRow +
@@ -760,7 +854,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
               }
             if (__any_sync(0xffffffffu, ((acc[0] | acc[1] | acc[2] | acc[3]) & 0x7fff7fffu) != 0)) {
 #pragma unroll 1
-              for (int s = 0; s < slots; ++s) {
+              for (int s = 0; s < last.slots; ++s) {
                 bool found = false;
 #pragma unroll 1
                 for (int hf = 0; hf < C::NH; ++hf)
@@ -774,7 +868,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
                     }
                   }
                 found = __any_sync(0xffffffffu, found);
-                const int who = __shfl_sync(0xffffffffu, owner, s);
+                const int who = __shfl_sync(0xffffffffu, last.owner, s);
                 if (found && lane == 0) {
                   const int n = dt->n;
                   if (n == 0 || n > kDirty || dt->seq[n - 1] != who) {
@@ -785,15 +879,26 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
               }
             }
           }
-          fence_async_shared();
-          mbar_arrive_lane0(v_ready + vr.i);
-          vr.next();
+          if (last.slots > 0) {
+            fence_async_shared();
+            mbar_arrive_lane0(v_ready + last.stage);
+          }
+          if (last.flags & TD_LAST) {
+            mbar_arrive_lane0(cleaned + unit % kUnitsAhead);
+            ++unit;
+          }
+          pending = false;
         }
-        if (flags & TD_LAST) {
-          mbar_arrive_lane0(cleaned + unit % kUnitsAhead);
-          ++unit;
+        if (issued) {
+          last = next;
+          pending = true;
         }
+        if (end && !pending) break;
       }
+      // (after a timed-out wait, the loads still on their way)
+      cp_async_wait();
+      if (!ok && pending && (last.flags & TD_FULL)) mbar_landed(v_full + last.stage, (full >> last.stage) & 1u, status);
+      if (!ok && issued && (next.flags & TD_FULL)) mbar_landed(v_full + next.stage, (full >> next.stage) & 1u, status);
     } else {
       // ---------------- queries ----------------
       Ring<2> ur;
@@ -1468,8 +1573,7 @@ extern "C" int fe_prefix_attention(const fe_prefix_args* a, void* stream) {
   p.scale = a->scale;
   p.sc = std::fmax((float)(a->scale * 1.4426950408889634), 1e-30f);
   PageMaps m;
-  if (!encode_pages(&m.k, a->kv, a->kv.k, kSlot) || !encode_pages(&m.v, a->kv, a->kv.v, kSlot) ||
-      !encode_pages(&m.k_page, a->kv, a->kv.k, p.page_rows) || !encode_pages(&m.v_page, a->kv, a->kv.v, p.page_rows))
+  if (!encode_pages(&m.k, a->kv, a->kv.k, p.page_rows) || !encode_pages(&m.v, a->kv, a->kv.v, p.page_rows))
     return fail(FE_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = a->kv.dtype == FE_IO_BF16 ? prefix_dim<__nv_bfloat16>(m, p, a->kv.head_dim, s)
