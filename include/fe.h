@@ -439,7 +439,7 @@ int fe_kv_append(const fe_append_args* args, void* stream);
  * prefix; the n_s = row_start[s + 1] - row_start[s] query rows of sequence s are the
  * last n_s of its own seq_len[s] rows (which the pages already hold), so the j-th sees
  * its own rows 0 .. seq_len[s] - n_s + j.  Query head h reads key head
- * h / (q_heads / kv_heads).
+ * h / (q_heads / kv_heads) (a whole number, at most 1024).
  *   out[t, h] = sum_k p_k v_k,  p = softmax(scale q . k) over the rows seen
  *   lse[t, h] = log sum_k exp(scale q . k)
  * A row that sees nothing gets out = 0 and lse = -inf.  Rows of the pages past a

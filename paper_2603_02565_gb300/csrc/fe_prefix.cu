@@ -59,11 +59,12 @@ struct PrefixParams {
   float* lse;
   int32_t* status;
   int64_t q_row, q_head;
-  int n_groups, n_seqs, n_rows, hq, hkv, hr, prefix_cols, page_cols, page_rows, page_shift, n_pages;
+  int n_groups, n_seqs, n_rows, hq, hkv, hr, hr_inv, prefix_cols, page_cols, page_rows, page_shift, n_pages;
   float scale, sc;  // sc: scale log2(e), and no 0 (masked scores, -inf, are multiplied by it)
   int ctas, max_tiles;
   // workspace
   PlanHead* head;
+  int2* tok;           // [n_rows] sequence of a row, and how many of its own rows it sees (-1: a length is none)
   int* gtile;          // [n_groups + 1] first row tile of a group
   long long* gcost;    // [n_groups + 1] key tiles of all heads before a group
   int* cost;           // [max_tiles] key tiles of a row tile (one head), at least 1
@@ -86,7 +87,7 @@ __device__ __forceinline__ int seen_rows(int len, int n, int j) { return max(0, 
 // ---------------------------------------------------------------------------
 // plan
 // ---------------------------------------------------------------------------
-constexpr int kPlanThreads = 1024, kPlanGroups = 4096;
+constexpr int kPlanThreads = 1024, kPlanGroups = 4096, kPlanCtas = 8;
 
 // inclusive sum over the block's threads
 template <typename V>
@@ -127,21 +128,28 @@ __device__ __forceinline__ int find_last(const V* a, int n, V x) {
   return lo;
 }
 
-__global__ void __launch_bounds__(kPlanThreads) prefix_plan_kernel(const PrefixParams p) {
+__device__ __forceinline__ void plan_barrier() {  // of the cluster, global writes included
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// One cluster: what is counted per sequence and row is spread over its CTAs, the sums over groups and row tiles are
+// the first one's.
+__global__ void __launch_bounds__(kPlanThreads) __cluster_dims__(kPlanCtas, 1, 1) prefix_plan_kernel(const PrefixParams p) {
   __shared__ long long sh[32];
   __shared__ int sh_i[32];
   __shared__ int sh_groups[kPlanGroups];
   pdl_trigger();
   pdl_wait();
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, all = blockIdx.x * kPlanThreads + tid;
+  constexpr int kAll = kPlanThreads * kPlanCtas;
   // offsets that are not increasing from 0 to their ends would send rows nowhere
   bool bad = p.row_start[0] != 0 || p.row_start[p.n_seqs] != p.n_rows || p.group_start[0] != 0 ||
              p.group_start[p.n_groups] != p.n_seqs;
+  for (int g = tid; g < p.n_groups; g += kPlanThreads) bad |= p.group_start[g] > p.group_start[g + 1];
 #pragma unroll 4
   for (int s = tid; s < p.n_seqs; s += kPlanThreads) bad |= p.row_start[s] > p.row_start[s + 1];
-  for (int g = tid; g < p.n_groups; g += kPlanThreads) bad |= p.group_start[g] > p.group_start[g + 1];
-  bad = __syncthreads_or(bad);
-  if (tid == 0) *p.head = PlanHead{0, bad ? 1 : 0, 0, 0};
+  bad = __syncthreads_or(bad);  // (the same in every CTA)
+  if (all == 0) *p.head = PlanHead{0, bad ? 1 : 0, 0, 0};
   if (bad) return;
   // (the groups' first sequences are searched for every sequence: in shared memory, if they fit)
   const int32_t* groups = p.group_start;
@@ -150,36 +158,41 @@ __global__ void __launch_bounds__(kPlanThreads) prefix_plan_kernel(const PrefixP
     groups = sh_groups;
     __syncthreads();
   }
-  // row tiles of the groups
-  int base = 0;
+  // row tiles of the groups (every CTA sums them up for itself, the first one writes them)
+  int tiles = 0;
   for (int g0 = 0; g0 < p.n_groups; g0 += kPlanThreads) {
     const int g = g0 + tid;
     int n = 0;
     if (g < p.n_groups) {
-      const long long rows = (long long)(p.row_start[p.group_start[g + 1]] - p.row_start[p.group_start[g]]) * p.hr;
+      const long long rows = (long long)(p.row_start[p.group_start[g + 1]] - p.row_start[groups[g]]) * p.hr;
       n = (int)((rows + kUnitRows - 1) / kUnitRows);
     }
     const int incl = block_scan(n, sh_i);
-    if (g < p.n_groups) p.gtile[g] = base + incl - n;
+    if (g < p.n_groups && blockIdx.x == 0) p.gtile[g] = tiles + incl - n;
     __syncthreads();
-    base += sh_i[31];
+    tiles += sh_i[31];
     __syncthreads();
   }
-  const int tiles = base;
-  if (tid == 0) {
+  if (all == 0) {
     p.gtile[p.n_groups] = tiles;
     p.head->n_tiles = tiles;
   }
-  for (int i = tid; i < tiles; i += kPlanThreads) p.cost[i] = 0;
-  __syncthreads();
+  for (int i = all; i < tiles; i += kAll) p.cost[i] = 0;
+  // what the rows see
+  for (int t = all; t < p.n_rows; t += kAll) {
+    const int s = find_last(p.row_start, p.n_seqs, t), a = p.row_start[s], len = p.seq_len[s];
+    const int g = find_last(groups, p.n_groups, s);
+    const bool fine = len_ok(p, len) && prefix_ok(p, p.prefix_len[g]);
+    p.tok[t] = make_int2(s, fine ? seen_rows(len, p.row_start[s + 1] - a, t - a) : -1);
+  }
+  plan_barrier();
   // slots of own keys: a sequence's first row tile by the sequence, its further ones by the tile
-  auto slots = [&](int s, int a, int n, int first, int i) {  // sequence s (rows a .. of the group's first, n of them) in tile i
+  auto slots = [&](int s, int a, int n, int first, int i) {  // sequence s (its n rows from a on, the group's from first on) in tile i
     const int len = p.seq_len[s];
     const int j = min(n - 1, (int)(((long long)(i + 1) * kUnitRows - 1) / p.hr) - (a - first));
     return len_ok(p, len) ? (seen_rows(len, n, j) + kSlot - 1) / kSlot : 0;
   };
-#pragma unroll 4
-  for (int s = tid; s < p.n_seqs; s += kPlanThreads) {
+  for (int s = all; s < p.n_seqs; s += kAll) {
     const int a = p.row_start[s], n = p.row_start[s + 1] - a;
     if (n == 0) continue;
     const int g = find_last(groups, p.n_groups, s), first = p.row_start[groups[g]];
@@ -187,17 +200,18 @@ __global__ void __launch_bounds__(kPlanThreads) prefix_plan_kernel(const PrefixP
     const int c = slots(s, a, n, first, i);
     if (c) atomicAdd(p.cost + p.gtile[g] + i, c);
   }
-  for (int rt = tid; rt < tiles; rt += kPlanThreads) {
+  for (int rt = all; rt < tiles; rt += kAll) {
     const int g = find_last(p.gtile, p.n_groups, rt), i = rt - p.gtile[g];
     if (i == 0) continue;
-    const int first = p.row_start[p.group_start[g]], t = first + (int)((long long)i * kUnitRows / p.hr);
+    const int first = p.row_start[groups[g]], t = first + (int)((long long)i * kUnitRows / p.hr);
     const int s = find_last(p.row_start, p.n_seqs, t), a = p.row_start[s];
     if ((long long)(a - first) * p.hr / kUnitRows < i) {
       const int c = slots(s, a, p.row_start[s + 1] - a, first, i);
       if (c) atomicAdd(p.cost + rt, c);
     }
   }
-  __syncthreads();
+  plan_barrier();
+  if (blockIdx.x != 0) return;
   // key tiles of the row tiles, and those before them
   long long run = 0;
   for (int r0 = 0; r0 < tiles; r0 += kPlanThreads) {
@@ -205,7 +219,8 @@ __global__ void __launch_bounds__(kPlanThreads) prefix_plan_kernel(const PrefixP
     long long c = 0;
     if (rt < tiles) {
       const int g = find_last(p.gtile, p.n_groups, rt), n = p.prefix_len[g];
-      c = ((prefix_ok(p, n) ? n : 0) + kTileKeys - 1) / kTileKeys + (p.cost[rt] + kSlots - 1) / kSlots;
+      const int own = *reinterpret_cast<volatile int*>(p.cost + rt);  // (summed in L2)
+      c = ((prefix_ok(p, n) ? n : 0) + kTileKeys - 1) / kTileKeys + (own + kSlots - 1) / kSlots;
       c = c < 1 ? 1 : c;
       p.cost[rt] = (int)c;
     }
@@ -251,7 +266,7 @@ struct PageMaps {
 
 template <int D>
 struct PrefixCfg {
-  static constexpr int kThreads = 384;
+  static constexpr int kThreads = 512;
   static constexpr uint32_t kRow = D >= 64 ? 128 : 64;  // bytes of a swizzled row
   static constexpr int NH = D == 128 ? 2 : 1;           // column halves of a tile
   static constexpr uint32_t kHalf = 128 * kRow, kTile = NH * kHalf;
@@ -262,8 +277,8 @@ struct PrefixCfg {
   static constexpr uint32_t kS = 0, kP = kOwnP ? 256 : 0, kPStep = kOwnP ? 64 : 128, kO = kOwnP ? 384 : 256;
   static_assert(kO + 2 * D <= 512, "TMEM budget");
   static constexpr int ND = 6;  // tile descriptors in flight
-  static constexpr int kBars = 3 * NV + 2 * NK + 2 * ND + 2 * 4 + 2 * 3 + 16 + kUnitsAhead + 1;
-  static constexpr size_t kFixed = sizeof(TileDesc) * ND + sizeof(UnitInfo) * 2 + sizeof(RowInfo) * 256 +
+  static constexpr int kBars = 3 * NV + 2 * NK + 2 * ND + 2 * 5 + 2 * 3 + 16 + kUnitsAhead + 2;
+  static constexpr size_t kFixed = sizeof(TileDesc) * ND + sizeof(UnitInfo) * 2 + sizeof(RowInfo) * 512 +
                                    sizeof(float2) * 256 + sizeof(Dirty) * kUnitsAhead + 8 * kBars + 16;
   static_assert(ND < kUnitsAhead, "a unit's dirty sequences are read before the entry is used again");
   static constexpr size_t kSmem = 1024 + (size_t)(2 + NK + NV) * kTile + kFixed;
@@ -383,26 +398,29 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
   uint8_t* sV = sK + NK * C::kTile;      // [NV]
   TileDesc* descs = reinterpret_cast<TileDesc*>(sV + NV * C::kTile);
   UnitInfo* units = reinterpret_cast<UnitInfo*>(descs + ND);
-  RowInfo* rinfo = reinterpret_cast<RowInfo*>(units + 2);       // [2][128]
-  float2* s_ml = reinterpret_cast<float2*>(rinfo + 256);        // [2][128]
+  RowInfo* rinfo = reinterpret_cast<RowInfo*>(units + 2);       // [2][256]
+  float2* s_ml = reinterpret_cast<float2*>(rinfo + 512);        // [2][128]
   Dirty* dirty = reinterpret_cast<Dirty*>(s_ml + 256);          // [kUnitsAhead]
   uint64_t* bars = reinterpret_cast<uint64_t*>(dirty + kUnitsAhead);
   uint64_t *k_full = bars, *k_empty = k_full + NK;
   uint64_t *v_full = k_empty + NK, *v_ready = v_full + NV, *v_empty = v_ready + NV;
   uint64_t *d_full = v_empty + NV, *d_empty = d_full + ND;
   uint64_t *s_full = d_empty + ND, *p_full = s_full + 2, *pv_done = p_full + 2;  // [2] by softmax group
-  uint64_t *u_full = pv_done + 2, *u_empty = u_full + 2, *q_full = u_empty + 2, *q_free = q_full + 2;  // [2]
-  uint64_t *x_full = q_free + 2, *x_read = x_full + 8;  // [2][4] exchange between the groups' warps
-  uint64_t *cleaned = x_read + 8, *drain = cleaned + kUnitsAhead;  // [kUnitsAhead] a unit's values are clean
+  uint64_t *u_full = pv_done + 2, *u_empty = u_full + 2, *q_full = u_empty + 2, *q_free = q_full + 2, *r_free = q_free + 2;  // [2]
+  uint64_t *x_full = r_free + 2, *x_read = x_full + 8;  // [2][4] exchange between the groups' warps
+  uint64_t *cleaned = x_read + 8, *drain = cleaned + kUnitsAhead;  // [kUnitsAhead] a unit's values are clean; [2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kBars; ++i) mbar_init(bars + i, 1);
-    for (int i = 0; i < ND; ++i) mbar_init(d_empty + i, 10);  // 8 softmax warps, the issuer, the cleaner
+    for (int i = 0; i < ND; ++i) mbar_init(d_empty + i, 12);  // 8 softmax warps, 2 issuers, 2 loaders
+    for (int i = 0; i < NK; ++i) mbar_init(k_empty + i, 2);  // both issuers, or one twice
+    for (int i = 0; i < NV; ++i) mbar_init(v_empty + i, 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(p_full + i, 4);
       mbar_init(q_free + i, 8);
+      mbar_init(r_free + i, 8);
     }
     fence_mbar_init();
     prefetch_tmap(&maps.k);
@@ -417,11 +435,10 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
   pdl_wait();
   int* status = &p.head->status;
 
-  if (warp < 4) {
+  if (warp < 4 || warp >= 12) {
     if (warp == 0) {
-      // ---------------- schedule and keys ----------------
+      // ---------------- schedule ----------------
       const int cta = blockIdx.x;
-      const uint32_t go = elect_one();
       const bool bad_plan = p.head->bad != 0;
       const long long total = bad_plan ? 0 : p.gcost[p.n_groups];
       // (no more CTAs than tiles: each of them has one at least)
@@ -431,30 +448,10 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       auto begin = [&](int c) { return each * c + min(c, more); };
       const long long hi = cta < ctas ? begin(cta + 1) : 0;
       long long x = cta < ctas ? begin(cta) : 0;
-      Ring<NK> kr;
       Ring<ND> dr;
       Ring<2> ur;
       bool ok = true;
       SplitRec rec = {};
-      // Slots on their way by cp.async, oldest first: their tiles are announced once they have landed, at the latest
-      // before this warp waits for anything.
-      int away = 0;
-      uint64_t *away0 = nullptr, *away1 = nullptr;
-      auto landed = [&](bool all) {
-        if (all)
-          cp_async_wait_group<0>();
-        else
-          cp_async_wait_group<2>();
-        fence_async_shared();
-        mbar_arrive_lane0(away0);
-        if (all && away == 2) mbar_arrive_lane0(away1);
-        away0 = away1;
-        away = all ? 0 : away - 1;
-      };
-      auto wait = [&](uint64_t* bar, uint32_t par) {
-        if (away && !there(bar, par)) landed(true);
-        return mbar_wait_ok(bar, par, status);
-      };
       // the unit that holds tile x: group, head, row tile; the next ones follow step by step
       int g = 0, head = 0, ti = 0, off = 0, first_rt = 0, n_rt = 0, s0 = 0, s1 = 0, t0 = 0, group_rows = 0, plen = 0;
       auto open_group = [&]() {
@@ -491,7 +488,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           rec = SplitRec{c - cta - 1, t0, r0, rows, head, {}};
         }
         // tell the query loader
-        if (!(ok = wait(u_empty + ur.i, ur.par ^ 1u))) break;
+        if (!(ok = mbar_wait_ok(u_empty + ur.i, ur.par ^ 1u, status))) break;
         if (lane == 0) units[ur.i] = UnitInfo{t0, r0, rows, head, both, g, 0, 0};
         mbar_arrive_lane0(u_full + ur.i);
         const int entry = ur.i;
@@ -589,7 +586,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           const uint32_t badm = __ballot_sync(0xffffffffu, mine && b_bad), part_m = __ballot_sync(0xffffffffu, mine && b_owner != -2 && b_count < kSlot);
           const int slots = __popc(used);
           const bool whole = part == 0 && slots == kSlots && part_m == 0 && badm == 0;
-          if (!(ok = wait(d_empty + dr.i, dr.par ^ 1u))) break;
+          if (!(ok = mbar_wait_ok(d_empty + dr.i, dr.par ^ 1u, status))) break;
           TileDesc* td = descs + dr.i;
           if (mine) {
             td->owner[lane - l0] = b_owner;
@@ -608,19 +605,6 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           }
           mbar_arrive_lane0(d_full + dr.i);
           dr.next();
-          if (slots == 0) continue;
-          if (!(ok = wait(k_empty + kr.i, kr.par ^ 1u))) break;
-          if (whole) {
-            load_pages<D>(sK + kr.i * C::kTile, &maps.k, k_full + kr.i, b_row, l0, p.page_rows, go);
-            cp_async_commit();
-          } else {
-            load_slots<D, false>(sK + kr.i * C::kTile, p.k, slots, b_row, b_count, l0);
-            cp_async_commit();
-            if (away == 2) landed(false);
-            (away ? away1 : away0) = k_full + kr.i;
-            ++away;
-          }
-          kr.next();
         }
         // the next unit: row tile, head, group with rows
         off = 0;
@@ -635,7 +619,6 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           }
         }
       }
-      if (away) landed(true);
       if (ok && mbar_wait_ok(d_empty + dr.i, dr.par ^ 1u, status)) {
         if (lane == 0) descs[dr.i].flags = TD_END;
         mbar_arrive_lane0(d_full + dr.i);
@@ -645,10 +628,58 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         }
       }
       if (lane == 0) p.recs[cta] = rec;
+    } else if (warp == 13) {
+      // ---------------- keys ----------------
+      const uint32_t go = elect_one();
+      Ring<NK> kr;
+      Ring<ND> dr;
+      // Slots on their way by cp.async, oldest first: their tiles are announced once they have landed, at the latest
+      // before this warp waits for anything.
+      int away = 0;
+      uint64_t *away0 = nullptr, *away1 = nullptr;
+      auto landed = [&](bool all) {
+        if (all)
+          cp_async_wait_group<0>();
+        else
+          cp_async_wait_group<2>();
+        fence_async_shared();
+        mbar_arrive_lane0(away0);
+        if (all && away == 2) mbar_arrive_lane0(away1);
+        away0 = away1;
+        away = all ? 0 : away - 1;
+      };
+      auto wait = [&](uint64_t* bar, uint32_t par) {
+        if (away && !there(bar, par)) landed(true);
+        return mbar_wait_ok(bar, par, status);
+      };
+      while (true) {
+        if (!wait(d_full + dr.i, dr.par)) break;
+        const TileDesc* td = descs + dr.i;
+        const int flags = td->flags, slots = td->slots, row = td->row[lane & (kSlots - 1)], count = td->count[lane & (kSlots - 1)];
+        if (flags & TD_END) break;
+        mbar_arrive_lane0(d_empty + dr.i);
+        dr.next();
+        if (slots == 0) continue;
+        if (!wait(k_empty + kr.i, kr.par ^ 1u)) break;
+        uint8_t* k = sK + kr.i * C::kTile;
+        if (flags & TD_FULL) {
+          load_pages<D>(k, &maps.k, k_full + kr.i, row, 0, p.page_rows, go);
+          cp_async_commit();
+        } else {
+          load_slots<D, false>(k, p.k, slots, row, count, 0);
+          cp_async_commit();
+          if (away == 2) landed(false);
+          (away ? away1 : away0) = k_full + kr.i;
+          ++away;
+        }
+        kr.next();
+      }
+      if (away) landed(true);
       // the loads land before the shared memory goes away, whatever became of their readers
       mbar_landed_ring(k_full, kr.i, kr.par ^ 1u, NK, status);
-    } else if (warp == 1) {
-      // ---------------- products ----------------
+    } else if (warp == 1 || warp == 12) {
+      // ---------------- products of one softmax group ----------------
+      const int w = warp == 12;
       const uint32_t go = elect_one();
       constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u;
       const uint32_t idesc = (1u << 4) | kType | (8u << 24);
@@ -656,128 +687,111 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       const uint64_t qd0 = tile_desc(smem_u32(sQ), 16, 8 * C::kRow, C::kSwz);
       const uint64_t kd0 = tile_desc(smem_u32(sK), 16, 8 * C::kRow, C::kSwz);
       const uint64_t vd0 = tile_desc(smem_u32(sV), C::kHalf, 8 * C::kRow, C::kSwz);
+      const uint32_t t_s = tmem + C::kS + (uint32_t)(w * 128), t_p = tmem + C::kP + (uint32_t)w * C::kPStep;
+      const uint32_t t_o = tmem + C::kO + (uint32_t)(w * D);
       Ring<NK> kr;
       Ring<NV> vr;
       Ring<ND> dr;
-      // A group's job whose product with V is still to come (slots 0: none), and how many it has finished
-      struct Job {
-        int slots, first, shared, vi;
-        uint32_t vpar, done;
-      };
-      Job a = {}, b = {};
-      uint32_t qpars = 0;                 // parities of the query entries, bit e
-      int opened = 0;                     // groups with a product in this unit's output, bit w
-      int flags = 0, slots = 0, entry = 0;  // the tile in hand; left: jobs it still has
-      int left = 0;
-      uint32_t half = 0;  // stages of V that one of their tile's two jobs has been finished with
-      bool end = false, need_q = false, need_k = false;  // what the tile in hand still waits for
-      int due = 0;                                       // the group that takes the next job
-      // The groups take jobs in turn; what is ready is issued, a group's product with V before its next scores.
-      // Nothing is waited for while something else could be issued: a tile's keys, its values, its queries' space and
-      // the groups' weights come in any order, and some only after what else is ready has been issued.
-      uint32_t idle = 0;
-      uint64_t since = 0;
+      uint32_t qpars = 0, jobs = 0;  // query entries' parities, bit e; jobs whose S has been issued
+      int jp = 0;                    // the group that takes the next job
+      bool opened = false;           // this unit's output has a product
+      // the last job, if its product with V is still to come (slots 0: it is not)
+      int p_slots = 0, p_first = 0, p_both = 0, p_vi = 0;
+      uint32_t p_vpar = 0;
+      // the tile in hand: what is waited for next, its description (0), its unit's queries (1), its keys (2), or
+      // nothing any more (3)
+      int need = 0, flags = 0, slots = 0, entry = 0;
+      bool ok = true;
 #pragma unroll 1
       while (true) {
-        bool progress = false;
-#pragma unroll 1
-        for (int e = 0; e < 2; ++e) {  // O += P V of a group's job, the older one first
-          const int w = due ^ e;
-          Job b_ = w ? b : a;
-          if (!b_.slots || !there(p_full + w, b_.done & 1u) || !there(v_ready + b_.vi, b_.vpar)) continue;
+        uint64_t* bar = need == 0 ? d_full + dr.i : need == 1 ? q_full + entry : k_full + kr.i;
+        const uint32_t par = need == 0 ? dr.par : need == 1 ? (qpars >> entry) & 1u : kr.par;
+        // O += P V, before the next scores (they go where the last ones, or P, are), and before waiting for what may
+        // only come after it (a stage of V, the queries' space)
+        if (p_slots && (need >= 2 || !there(bar, par))) {
+          if (!(ok = mbar_wait_ok(p_full + w, (jobs - 1) & 1u, status))) break;
+          if (!(ok = mbar_wait_ok(v_ready + p_vi, p_vpar, status))) break;
           tc_fence_after();
-          const uint32_t o = tmem + C::kO + (uint32_t)(w * D), pa = tmem + C::kP + (uint32_t)w * C::kPStep;
-          const uint64_t vd = vd0 + (uint64_t)((b_.vi * C::kTile) >> 4);
-          umma_bf16_tmem_a_if(o, pa, vd, idesc_pv, b_.first ? 0u : 1u, go);
-          if (b_.slots == kSlots) {
+          const uint64_t vd = vd0 + (uint64_t)((p_vi * C::kTile) >> 4);
+          umma_bf16_tmem_a_if(t_o, t_p, vd, idesc_pv, p_first ? 0u : 1u, go);
+          if (p_slots == kSlots) {
 #pragma unroll
             for (int s = 1; s < kSlots; ++s)
-              umma_bf16_tmem_a_if(o, pa + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv, 1u, go);
+              umma_bf16_tmem_a_if(t_o, t_p + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv, 1u, go);
           } else {
 #pragma unroll 1
-            for (int s = 1; s < b_.slots; ++s)
-              umma_bf16_tmem_a_if(o, pa + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv, 1u, go);
+            for (int s = 1; s < p_slots; ++s)
+              umma_bf16_tmem_a_if(t_o, t_p + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv, 1u, go);
           }
           umma_commit_if(pv_done + w, go);
-          // (two jobs of a tile, in either order: its values are free with the later one)
-          if (b_.shared) half ^= 1u << b_.vi;
-          if (!((half >> b_.vi) & 1u)) umma_commit_if(v_empty + b_.vi, go);
-          ++b_.done;
-          b_.slots = 0;
-          if (w)
-            b = b_;
-          else
-            a = b_;
-          progress = true;
+          umma_commit_if(v_empty + p_vi, go);
+          if (!p_both) umma_commit_if(v_empty + p_vi, go);
+          p_slots = 0;
         }
-        Job cur = due ? b : a;
-        if (!cur.slots && !end) {
-          if (left == 0 && !need_q && there(d_full + dr.i, dr.par)) {
-            const TileDesc* td = descs + dr.i;
-            flags = td->flags;
-            slots = td->slots;
-            entry = td->entry;
-            progress = true;
-            if (flags & TD_END) {
-              end = true;
-            } else {
-              mbar_arrive_lane0(d_empty + dr.i);
-              dr.next();
-              need_q = flags & TD_FIRST;
-              need_k = true;
-              left = slots == 0 ? 0 : flags & TD_BOTH ? 2 : 1;
-            }
+        if (need == 3) break;
+        if (!(ok = mbar_wait_ok(bar, par, status))) break;
+        if (need == 0) {
+          const TileDesc* td = descs + dr.i;
+          flags = td->flags;
+          slots = td->slots;
+          entry = td->entry;
+          if (flags & TD_END) {
+            need = 3;
+            continue;
           }
-          if (need_q && there(q_full + entry, (qpars >> entry) & 1u)) {
-            qpars ^= 1u << entry;
-            opened = 0;
-            need_q = false;
-            progress = true;
+          mbar_arrive_lane0(d_empty + dr.i);
+          dr.next();
+          need = 2;
+          if (flags & TD_FIRST) {
+            need = 1;
+            continue;
           }
-          if (need_k && left && there(k_full + kr.i, kr.par)) need_k = false;
-          // (without columns of its own, P lies where the next S goes)
-          if (left && !need_q && !need_k && (C::kOwnP || cur.done == 0 || there(pv_done + due, (cur.done - 1) & 1u))) {
-            tc_fence_after();
-            const int w = due;
-            const uint64_t qd = qd0 + (uint64_t)(((flags & TD_BOTH ? w : entry) * C::kTile) >> 4);
-            const uint64_t kd = kd0 + (uint64_t)((kr.i * C::kTile) >> 4);
-            const uint32_t id = idesc | ((uint32_t)(slots * 2) << 17);
+        } else if (need == 1) {
+          qpars ^= 1u << entry;
+          opened = false;
+          need = 2;
+        } else {
+          // (without columns of its own, P lies where these scores go)
+          if (!C::kOwnP && jobs > 0 && !(ok = mbar_wait_ok(pv_done + w, (jobs - 1) & 1u, status))) break;
+          tc_fence_after();
+          const bool both = flags & TD_BOTH;
+          const uint64_t qd = qd0 + (uint64_t)(((both ? w : entry) * C::kTile) >> 4);
+          const uint64_t kd = kd0 + (uint64_t)((kr.i * C::kTile) >> 4);
+          const uint32_t id = idesc | ((uint32_t)(slots * 2) << 17);
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-              const uint64_t at = (uint64_t)(((kk * 32) / C::kRow * C::kHalf + (kk * 32) % C::kRow) >> 4);
-              umma_bf16_if(tmem + C::kS + (uint32_t)(w * 128), qd + at, kd + at, id, kk != 0 ? 1u : 0u, go);
-            }
-            umma_commit_if(s_full + w, go);
-            --left;
-            if (left == 0) umma_commit_if(k_empty + kr.i, go);
-            cur = Job{slots, (opened >> w) & 1 ? 0 : 1, flags & TD_BOTH ? 1 : 0, vr.i, vr.par, cur.done};
-            opened |= 1 << w;
-            if (w)
-              b = cur;
-            else
-              a = cur;
-            if (left == 0) {
-              kr.next();
-              vr.next();
-            }
-            due ^= 1;
-            progress = true;
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint64_t at = (uint64_t)(((kk * 32) / C::kRow * C::kHalf + (kk * 32) % C::kRow) >> 4);
+            umma_bf16_if(t_s, qd + at, kd + at, id, kk != 0 ? 1u : 0u, go);
           }
+          umma_commit_if(s_full + w, go);
+          umma_commit_if(k_empty + kr.i, go);
+          if (!both) umma_commit_if(k_empty + kr.i, go);
+          ++jobs;
+          p_slots = slots;
+          p_first = !opened;
+          p_both = both;
+          p_vi = vr.i;
+          p_vpar = vr.par;
+          opened = true;
+          kr.next();
+          vr.next();
+          need = 0;
+          continue;
         }
-        if (end && !a.slots && !b.slots) break;
-        // bounded, as every wait
-        if (progress) {
-          idle = 0;
-        } else if ((++idle & 255u) == 0) {
-          const uint64_t now = globaltimer_ns();
-          if (idle == 256) since = now;
-          bool stop = now - since > (uint64_t)kWaitLimitUs * 1000u;
-          if (stop) atomicOr(status, ST_TIMEOUT);
-          stop = stop || (*reinterpret_cast<volatile int*>(status) & ST_TIMEOUT);
-          if (__any_sync(0xffffffffu, stop)) break;
+        // a tile without keys, or the other group's, is passed over
+        if (slots == 0) {
+          need = 0;
+        } else if (!(flags & TD_BOTH)) {
+          const bool mine = jp == w;
+          jp ^= 1;
+          if (!mine) {
+            kr.next();
+            vr.next();
+            need = 0;
+          }
         }
       }
-      umma_drain(drain, status, go);
+      umma_drain(drain + w, status, go);
     } else if (warp == 2) {
       // ---------------- values ----------------
       // A tile is loaded, and the one before it then made ready (or at once, while the next has to wait).
@@ -899,7 +913,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       cp_async_wait();
       if (!ok && pending && (last.flags & TD_FULL)) mbar_landed(v_full + last.stage, (full >> last.stage) & 1u, status);
       if (!ok && issued && (next.flags & TD_FULL)) mbar_landed(v_full + next.stage, (full >> next.stage) & 1u, status);
-    } else {
+    } else if (warp == 3) {
       // ---------------- queries ----------------
       Ring<2> ur;
       uint32_t uses[2] = {0, 0};
@@ -908,42 +922,52 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         const UnitInfo u = units[ur.i];
         if (u.end) break;
         const int e = ur.i;
+        const uint32_t ur_par = ur.par;
         mbar_arrive_lane0(u_empty + e);
         ur.next();
-        bool ok = true;
+        // what the rows see, sequence by sequence (before their queries' space is free)
+        bool ok = mbar_wait_ok(r_free + e, ur_par ^ 1u, status);
+        if (!ok) break;
+        const int t_first = u.r0 / p.hr, h_first = u.r0 - t_first * p.hr;  // the unit's first row: token, query head
+        auto at = [&](int r, int& t, int& h) {  // (a product instead of a division: exact below 2^16)
+          const int q = (int)__umulhi((uint32_t)(h_first + r), (uint32_t)p.hr_inv);
+          t = u.t0 + t_first + (p.hr == 1 ? r : q);
+          h = u.head * p.hr + (p.hr == 1 ? 0 : h_first + r - q * p.hr);
+        };
+        {
+          RowInfo* info = rinfo + e * 256;
+          int2 k[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            int t, h;
+            at(lane + 32 * i, t, h);
+            k[i] = lane + 32 * i < u.rows ? __ldg(p.tok + t) : make_int2(-5, 0);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            int t, h;
+            at(lane + 32 * i, t, h);
+            info[lane + 32 * i] = RowInfo{k[i].x, k[i].y, k[i].x < 0 ? -1 : t * p.hq + h, 0};
+          }
+        }
         const int h0 = u.both ? 0 : e, h1 = u.both ? 1 : e;
         for (int h = h0; h <= h1 && ok; ++h) {
           if (uses[h] > 0) ok = mbar_wait_ok(q_free + h, (uses[h] - 1) & 1u, status);
           ++uses[h];
         }
         if (!ok) break;
-        const int s0 = p.group_start[u.group], s1 = p.group_start[u.group + 1];
-        const bool pre_ok = prefix_ok(p, p.prefix_len[u.group]);
-        const int n = u.both ? 256 : 128;
         // the queries: pieces of 16 bytes, swizzled as TMA would have it
         constexpr int NP = D / 8, RP = 32 / NP;  // pieces of a row, rows of a step
         const int pc = lane % NP;
         const uint32_t hoff = (uint32_t)(pc * 16) / C::kRow * C::kHalf, poff = (uint32_t)(pc * 16) % C::kRow;
-#pragma unroll 2
+#pragma unroll 4
         for (int r = lane / NP; r < u.rows; r += RP) {
-          const int rr = u.r0 + r, t = u.t0 + rr / p.hr, h = u.head * p.hr + rr % p.hr;
+          int t, h;
+          at(r, t, h);
           const T* src = reinterpret_cast<const T*>(p.q) + (long long)t * p.q_row + h * p.q_head + pc * 8;
           const uint32_t row = (uint32_t)(r & 127);
           const uint32_t mask = C::kRow == 128 ? (row & 7u) : ((row >> 1) & 3u);
           cp_async16(smem_u32(sQ) + (uint32_t)((u.both ? r >> 7 : e) * C::kTile) + hoff + row * C::kRow + (poff ^ (mask << 4)), src);
-        }
-#pragma unroll 1
-        for (int r = lane; r < n; r += 32) {
-          RowInfo ri = {-5, 0, -1, 0};
-          if (r < u.rows) {
-            const int rr = u.r0 + r, t = u.t0 + rr / p.hr;
-            const int s = s0 + find_last(p.row_start + s0, s1 - s0, t), a = p.row_start[s];
-            const int len = p.seq_len[s];
-            ri.seq = s;
-            ri.seen = pre_ok && len_ok(p, len) ? seen_rows(len, p.row_start[s + 1] - a, t - a) : -1;
-            ri.out = t * p.hq + u.head * p.hr + rr % p.hr;
-          }
-          rinfo[(u.both ? 0 : e * 128) + r] = ri;
         }
         cp_async_wait();
         fence_async_shared();
@@ -979,7 +1003,8 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         qpars ^= 1u << entry;
         if (partner && !mbar_wait_ok(x_read + (1 - w) * 4 + qd, (joined - 1) & 1u, status)) break;
         partner = false;
-        ri = rinfo[(both ? w * 128 : entry * 128) + row];
+        ri = rinfo[entry * 256 + (both ? w * 128 : 0) + row];
+        mbar_arrive_lane0(r_free + entry);
         active = __any_sync(0xffffffffu, ri.seq >= 0);
         m = -INFINITY;
         l = 0.f;
@@ -1411,6 +1436,7 @@ int check_prefix(const fe_prefix_args* a) {
     return fail(FE_ERR_INVALID_ARG, "negative size or no page column");
   if (a->q_heads < 1 || a->q_heads % a->kv.kv_heads != 0)
     return fail(FE_ERR_INVALID_ARG, "q_heads must be a multiple of kv_heads");
+  if (a->q_heads / a->kv.kv_heads > 1024) return fail(FE_ERR_UNSUPPORTED, "at most 1024 query heads a key head");
   if ((long long)a->n_rows * a->q_heads > 0x7fffffffLL)
     return fail(FE_ERR_UNSUPPORTED, "n_rows * q_heads must be below 2^31");
   if (!std::isfinite(a->scale) || a->scale < 0.f) return fail(FE_ERR_INVALID_ARG, "scale must be finite and not negative");
@@ -1426,7 +1452,7 @@ int check_prefix(const fe_prefix_args* a) {
 
 // Sizes of the workspace's parts, in order, each on a 256-byte boundary
 struct Layout {
-  size_t head, gtile, gcost, cost, before, recs, list, part_o, part_ml, bytes;
+  size_t head, tok, gtile, gcost, cost, before, recs, list, part_o, part_ml, bytes;
 };
 Layout layout(const fe_prefix_args* a, int ctas, int max_tiles) {
   size_t at = 0;
@@ -1437,6 +1463,7 @@ Layout layout(const fe_prefix_args* a, int ctas, int max_tiles) {
   };
   Layout w;
   w.head = take(sizeof(PlanHead));
+  w.tok = take(8 * (size_t)a->n_rows);
   w.gtile = take(4 * ((size_t)a->n_groups + 1));
   w.gcost = take(8 * ((size_t)a->n_groups + 1));
   w.cost = take(4 * (size_t)max_tiles);
@@ -1497,7 +1524,7 @@ bool encode_pages(CUtensorMap* m, const fe_paged_kv& kv, const void* base, int r
 template <typename T, int D>
 cudaError_t prefix_go(const PageMaps& m, const PrefixParams& p, cudaStream_t s) {
   using C = PrefixCfg<D>;
-  cudaError_t e = launch_k(prefix_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, p);
+  cudaError_t e = launch_k(prefix_plan_kernel, dim3(kPlanCtas), dim3(kPlanThreads), 0, s, p);
   if (e == cudaSuccess)
     e = launch_k(prefix_attend_kernel<T, D>, dim3((unsigned)p.ctas), dim3(C::kThreads), C::kSmem, s, m, p);
   if (e == cudaSuccess) e = launch_k(prefix_finish_kernel<T, D>, dim3((unsigned)p.ctas, 8), dim3(256), 0, s, p);
@@ -1537,6 +1564,7 @@ extern "C" int fe_prefix_attention(const fe_prefix_args* a, void* stream) {
   if (a->workspace_bytes < w.bytes) return fail(FE_ERR_WORKSPACE, "workspace too small");
   char* ws = static_cast<char*>(a->workspace);
   p.head = reinterpret_cast<PlanHead*>(ws + w.head);
+  p.tok = reinterpret_cast<int2*>(ws + w.tok);
   p.gtile = reinterpret_cast<int*>(ws + w.gtile);
   p.gcost = reinterpret_cast<long long*>(ws + w.gcost);
   p.cost = reinterpret_cast<int*>(ws + w.cost);
@@ -1565,6 +1593,7 @@ extern "C" int fe_prefix_attention(const fe_prefix_args* a, void* stream) {
   p.hq = a->q_heads;
   p.hkv = a->kv.kv_heads;
   p.hr = p.hq / p.hkv;
+  p.hr_inv = (int)(uint32_t)((0x100000000ull + p.hr - 1) / p.hr);
   p.prefix_cols = a->prefix_cols;
   p.page_cols = a->page_cols;
   p.page_rows = a->kv.page_rows;
