@@ -5,23 +5,24 @@
 //   p_k = softmax_k(scale q . k) over the prefix's prefix_len[g] rows and the sequence's
 //   own rows 0 .. seq_len[s] - n_s + j,  out = sum_k p_k v_k.
 //
-// Unit of work: up to 256 query rows of a group that read the same key head (tokens x the
+// Unit of work: up to 128 query rows of a group that read the same key head (tokens x the
 // query heads of that key head), so that a prefix key is loaded once for all of them.
 // Its keys come in tiles of 128: first the prefix's, then the own rows of the unit's
 // sequences, packed in slots of 16 keys (a slot has one owner; a row masks the slots of
 // others), so short sequences share tiles and decoding needs no second kernel for them.
 //   plan kernel     counts each unit's tiles from the lengths in device memory;
-//   attend kernel   one CTA per SM takes an equal run of all units' tiles, wherever it
-//                   begins or ends: few units with long prefixes are split over the SMs;
+//   attend kernel   two CTAs per SM, each takes an equal run of all units' tiles, wherever
+//                   it begins or ends: few units with long prefixes are split over the SMs;
 //   finish kernel   joins the pieces of split units by their maxima and sums, and computes
 //                   some rows again, key by key (see below).
 //
-// In the attend kernel two groups of four softmax warps work on alternate jobs.  Up to
-// 128 query rows, a job is a key tile, and the groups' outputs are joined at the unit's
-// end; above, both groups take every tile, each with its own 128 rows.  One warp walks
-// the schedule and loads (TMA), one issues tcgen05.mma (S = Q K^T, and O += P V with P
-// from TMEM), one loads the next unit's queries, one cleans value tiles.  S, P and O live
-// in TMEM.
+// A CTA of the attend kernel has four softmax warps (a row a thread) and four that feed
+// them: one walks the schedule, one issues tcgen05.mma (S = Q K^T, and O += P V with P from
+// TMEM), one loads queries and keys, one loads values and looks through them.  S, P and O
+// live in half of the SM's TMEM.  What such a warp does is a chain of short steps, some
+// five cycles an instruction: the two CTAs fill each other's gaps.  (One CTA per SM with two
+// groups of softmax warps, on alternate tiles or on 256 rows, joined at the unit's end,
+// had the same steps in one chain for both.)
 //
 // 0 x NaN is NaN, so a value that is no number spoils rows that give it no weight.  The
 // cleaning warp clears the value rows past a sequence's end, whatever the pages hold there,
@@ -37,7 +38,7 @@
 namespace fe {
 namespace {
 
-constexpr int kUnitRows = 256, kTileKeys = 128, kSlot = 16, kSlots = kTileKeys / kSlot;
+constexpr int kUnitRows = 128, kTileKeys = 128, kSlot = 16, kSlots = kTileKeys / kSlot;
 constexpr int kListed = 1 << 16;  // rows to compute again that the list holds
 constexpr int kDirty = 3, kUnitsAhead = 8;
 
@@ -69,7 +70,7 @@ struct PrefixParams {
   long long* gcost;    // [n_groups + 1] key tiles of all heads before a group
   int* cost;           // [max_tiles] key tiles of a row tile (one head), at least 1
   long long* before;   // [max_tiles + 1] key tiles of one head before a row tile
-  SplitRec* recs;      // [ctas]
+  SplitRec* recs;      // [ctas] (two an SM)
   int* list;           // [kListed]
   float* part_o;       // [ctas][2][kUnitRows][D]
   float2* part_ml;     // [ctas][2][kUnitRows] maximum (log2 units) and sum
@@ -240,15 +241,15 @@ __global__ void __launch_bounds__(kPlanThreads) __cluster_dims__(kPlanCtas, 1, 1
 // ---------------------------------------------------------------------------
 // What the loading warp tells the others about a key tile
 struct alignas(16) TileDesc {
-  int flags, slots, bad, piece, entry, pad[3];
+  int flags, slots, bad, piece, pad[4];
   int owner[kSlots];  // sequence, or -1: the prefix
   int base[kSlots];   // the slot's first key
   int count[kSlots];  // its valid keys
   int row[kSlots];    // the first one's row of the pages
 };
-enum : int { TD_FIRST = 1, TD_LAST = 2, TD_BOTH = 4, TD_FULL = 8, TD_END = 16, TD_SCAN = 32 };
+enum : int { TD_FIRST = 1, TD_LAST = 2, TD_FULL = 4, TD_END = 8, TD_SCAN = 16 };
 struct UnitInfo {
-  int t0, r0, rows, head, both, group, end, pad;
+  int t0, r0, rows, head;  // first token of the group, first row and rows of the unit, its key head
 };
 struct RowInfo {
   int seq, seen, out, pad;  // sequence (-5: no row), own keys seen (-1: spoiled), row of the output
@@ -266,23 +267,24 @@ struct PageMaps {
 
 template <int D>
 struct PrefixCfg {
-  static constexpr int kThreads = 512;
+  static constexpr int kThreads = 256;
   static constexpr uint32_t kRow = D >= 64 ? 128 : 64;  // bytes of a swizzled row
   static constexpr int NH = D == 128 ? 2 : 1;           // column halves of a tile
   static constexpr uint32_t kHalf = 128 * kRow, kTile = NH * kHalf;
-  static constexpr int NK = D == 128 ? 2 : D == 64 ? 5 : 8, NV = NK;
+  // tiles of queries, keys and values in shared memory
+  static constexpr int NQ = D == 128 ? 1 : 2, NK = D == 128 ? 1 : D == 64 ? 2 : 4, NV = NK;
   static constexpr uint32_t kSwz = D >= 64 ? 2u : 4u;  // descriptor swizzle code (128 B / 64 B)
-  // TMEM columns: S of group w, P (its own columns where they fit), O
+  // TMEM columns: S, P (its own columns where they fit), O
   static constexpr bool kOwnP = D <= 64;
-  static constexpr uint32_t kS = 0, kP = kOwnP ? 256 : 0, kPStep = kOwnP ? 64 : 128, kO = kOwnP ? 384 : 256;
-  static_assert(kO + 2 * D <= 512, "TMEM budget");
+  static constexpr uint32_t kCols = 256, kP = kOwnP ? 128 : 0, kO = kOwnP ? 192 : 128;
+  static_assert(kO + D <= kCols, "TMEM budget");
   static constexpr int ND = 6;  // tile descriptors in flight
-  static constexpr int kBars = 3 * NV + 2 * NK + 2 * ND + 2 * 5 + 2 * 3 + 16 + kUnitsAhead + 2;
-  static constexpr size_t kFixed = sizeof(TileDesc) * ND + sizeof(UnitInfo) * 2 + sizeof(RowInfo) * 512 +
-                                   sizeof(float2) * 256 + sizeof(Dirty) * kUnitsAhead + 8 * kBars + 16;
-  static_assert(ND < kUnitsAhead, "a unit's dirty sequences are read before the entry is used again");
-  static constexpr size_t kSmem = 1024 + (size_t)(2 + NK + NV) * kTile + kFixed;
-  static_assert(kSmem <= 232448, "shared memory budget");
+  static constexpr int kBars = 3 * NV + 2 * NK + 2 * ND + 2 * NQ + 3 + kUnitsAhead + 1;
+  static constexpr size_t kFixed = sizeof(TileDesc) * ND + sizeof(UnitInfo) * kUnitsAhead + sizeof(RowInfo) * 128 * NQ +
+                                   sizeof(Dirty) * kUnitsAhead + 8 * kBars + 16;
+  static_assert(ND < kUnitsAhead, "a unit's entries are read before they are used again");
+  static constexpr size_t kSmem = 1024 + (size_t)(NQ + NK + NV) * kTile + kFixed;
+  static_assert(kSmem <= 115000, "two CTAs an SM");
 };
 
 __device__ __forceinline__ uint64_t tile_desc(uint32_t saddr, uint32_t lbo, uint32_t sbo, uint32_t swz) {
@@ -387,46 +389,38 @@ __device__ __forceinline__ float maxn(const float* v) {
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
+__global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
     prefix_attend_kernel(const __grid_constant__ PageMaps maps, const PrefixParams p) {
   using C = PrefixCfg<D>;
-  constexpr int NK = C::NK, NV = C::NV, ND = C::ND;
+  constexpr int NQ = C::NQ, NK = C::NK, NV = C::NV, ND = C::ND;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint8_t* sQ = smem;                    // [2] halves of 128 rows
-  uint8_t* sK = sQ + 2 * C::kTile;       // [NK]
-  uint8_t* sV = sK + NK * C::kTile;      // [NV]
+  uint8_t* sQ = smem;                   // [NQ]
+  uint8_t* sK = sQ + NQ * C::kTile;     // [NK]
+  uint8_t* sV = sK + NK * C::kTile;     // [NV]
   TileDesc* descs = reinterpret_cast<TileDesc*>(sV + NV * C::kTile);
-  UnitInfo* units = reinterpret_cast<UnitInfo*>(descs + ND);
-  RowInfo* rinfo = reinterpret_cast<RowInfo*>(units + 2);       // [2][256]
-  float2* s_ml = reinterpret_cast<float2*>(rinfo + 512);        // [2][128]
-  Dirty* dirty = reinterpret_cast<Dirty*>(s_ml + 256);          // [kUnitsAhead]
+  UnitInfo* units = reinterpret_cast<UnitInfo*>(descs + ND);       // [kUnitsAhead]
+  RowInfo* rinfo = reinterpret_cast<RowInfo*>(units + kUnitsAhead);  // [NQ][128]
+  Dirty* dirty = reinterpret_cast<Dirty*>(rinfo + 128 * NQ);       // [kUnitsAhead]
   uint64_t* bars = reinterpret_cast<uint64_t*>(dirty + kUnitsAhead);
   uint64_t *k_full = bars, *k_empty = k_full + NK;
   uint64_t *v_full = k_empty + NK, *v_ready = v_full + NV, *v_empty = v_ready + NV;
-  uint64_t *d_full = v_empty + NV, *d_empty = d_full + ND;
-  uint64_t *s_full = d_empty + ND, *p_full = s_full + 2, *pv_done = p_full + 2;  // [2] by softmax group
-  uint64_t *u_full = pv_done + 2, *u_empty = u_full + 2, *q_full = u_empty + 2, *q_free = q_full + 2, *r_free = q_free + 2;  // [2]
-  uint64_t *x_full = r_free + 2, *x_read = x_full + 8;  // [2][4] exchange between the groups' warps
-  uint64_t *cleaned = x_read + 8, *drain = cleaned + kUnitsAhead;  // [kUnitsAhead] a unit's values are clean; [2]
+  uint64_t *d_full = v_empty + NV, *d_empty = d_full + ND, *q_full = d_empty + ND, *q_free = q_full + NQ;
+  uint64_t *s_full = q_free + NQ, *p_full = s_full + 1, *pv_done = s_full + 2;
+  uint64_t *cleaned = s_full + 3, *drain = cleaned + kUnitsAhead;  // [kUnitsAhead] a unit's values have been looked through
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + C::kBars);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kBars; ++i) mbar_init(bars + i, 1);
-    for (int i = 0; i < ND; ++i) mbar_init(d_empty + i, 12);  // 8 softmax warps, 2 issuers, 2 loaders
-    for (int i = 0; i < NK; ++i) mbar_init(k_empty + i, 2);  // both issuers, or one twice
-    for (int i = 0; i < NV; ++i) mbar_init(v_empty + i, 2);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(p_full + i, 4);
-      mbar_init(q_free + i, 8);
-      mbar_init(r_free + i, 8);
-    }
+    for (int i = 0; i < ND; ++i) mbar_init(d_empty + i, 7);  // all warps but the schedule's
+    for (int i = 0; i < NQ; ++i) mbar_init(q_free + i, 4);
+    mbar_init(p_full, 4);
     fence_mbar_init();
     prefetch_tmap(&maps.k);
     prefetch_tmap(&maps.v);
   }
-  if (warp == 1) tmem_alloc(tmem_slot, 512);
+  if (warp == 1) tmem_alloc(tmem_slot, C::kCols);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -435,7 +429,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
   pdl_wait();
   int* status = &p.head->status;
 
-  if (warp < 4 || warp >= 12) {
+  if (warp < 4) {
     if (warp == 0) {
       // ---------------- schedule ----------------
       const int cta = blockIdx.x;
@@ -449,9 +443,9 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       const long long hi = cta < ctas ? begin(cta + 1) : 0;
       long long x = cta < ctas ? begin(cta) : 0;
       Ring<ND> dr;
-      Ring<2> ur;
       bool ok = true;
       SplitRec rec = {};
+      uint32_t unit = 0;
       // the unit that holds tile x: group, head, row tile; the next ones follow step by step
       int g = 0, head = 0, ti = 0, off = 0, first_rt = 0, n_rt = 0, s0 = 0, s1 = 0, t0 = 0, group_rows = 0, plen = 0;
       auto open_group = [&]() {
@@ -478,7 +472,6 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         const int cost = p.cost[first_rt + ti];
         const int n = (int)min((long long)(cost - off), hi - x);
         const int r0 = ti * kUnitRows, rows = min(kUnitRows, group_rows - r0);
-        const int both = rows > 128;
         const int piece = off == 0 && n == cost ? -1 : off == 0 ? 1 : 0;
         if (piece == 1) {  // further pieces: the CTAs that begin inside the unit
           const long long end = x + cost;
@@ -487,12 +480,8 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           while (c < ctas && begin(c) < end) ++c;
           rec = SplitRec{c - cta - 1, t0, r0, rows, head, {}};
         }
-        // tell the query loader
-        if (!(ok = mbar_wait_ok(u_empty + ur.i, ur.par ^ 1u, status))) break;
-        if (lane == 0) units[ur.i] = UnitInfo{t0, r0, rows, head, both, g, 0, 0};
-        mbar_arrive_lane0(u_full + ur.i);
-        const int entry = ur.i;
-        ur.next();
+        // (each reader of a unit's entry reads it before it passes on the unit's first tile)
+        const UnitInfo info = {t0, r0, rows, head};
         const int ptiles = (plen + kTileKeys - 1) / kTileKeys;
         // own keys: the sequences of the unit's rows, 32 at a time, with their first slots
         const int ta = t0 + r0 / p.hr, tb = t0 + (r0 + rows - 1) / p.hr;
@@ -595,17 +584,18 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
             td->row[lane - l0] = b_row;
           }
           if (lane == 0) {
-            td->flags = (j == off ? TD_FIRST : 0) | (j == off + n - 1 ? TD_LAST : 0) | (both ? TD_BOTH : 0) |
+            if (j == off) units[unit % kUnitsAhead] = info;
+            td->flags = (j == off ? TD_FIRST : 0) | (j == off + n - 1 ? TD_LAST : 0) |
                         (whole ? TD_FULL : 0) |
                         (part == 1 && ta != tb ? TD_SCAN : 0);
             td->slots = slots;
             td->bad = (int)(badm >> l0);
             td->piece = piece;
-            td->entry = entry;
           }
           mbar_arrive_lane0(d_full + dr.i);
           dr.next();
         }
+        ++unit;
         // the next unit: row tile, head, group with rows
         off = 0;
         if (x < hi && ++ti == n_rt) {
@@ -622,64 +612,10 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       if (ok && mbar_wait_ok(d_empty + dr.i, dr.par ^ 1u, status)) {
         if (lane == 0) descs[dr.i].flags = TD_END;
         mbar_arrive_lane0(d_full + dr.i);
-        if (mbar_wait_ok(u_empty + ur.i, ur.par ^ 1u, status)) {
-          if (lane == 0) units[ur.i].end = 1;
-          mbar_arrive_lane0(u_full + ur.i);
-        }
       }
       if (lane == 0) p.recs[cta] = rec;
-    } else if (warp == 13) {
-      // ---------------- keys ----------------
-      const uint32_t go = elect_one();
-      Ring<NK> kr;
-      Ring<ND> dr;
-      // Slots on their way by cp.async, oldest first: their tiles are announced once they have landed, at the latest
-      // before this warp waits for anything.
-      int away = 0;
-      uint64_t *away0 = nullptr, *away1 = nullptr;
-      auto landed = [&](bool all) {
-        if (all)
-          cp_async_wait_group<0>();
-        else
-          cp_async_wait_group<2>();
-        fence_async_shared();
-        mbar_arrive_lane0(away0);
-        if (all && away == 2) mbar_arrive_lane0(away1);
-        away0 = away1;
-        away = all ? 0 : away - 1;
-      };
-      auto wait = [&](uint64_t* bar, uint32_t par) {
-        if (away && !there(bar, par)) landed(true);
-        return mbar_wait_ok(bar, par, status);
-      };
-      while (true) {
-        if (!wait(d_full + dr.i, dr.par)) break;
-        const TileDesc* td = descs + dr.i;
-        const int flags = td->flags, slots = td->slots, row = td->row[lane & (kSlots - 1)], count = td->count[lane & (kSlots - 1)];
-        if (flags & TD_END) break;
-        mbar_arrive_lane0(d_empty + dr.i);
-        dr.next();
-        if (slots == 0) continue;
-        if (!wait(k_empty + kr.i, kr.par ^ 1u)) break;
-        uint8_t* k = sK + kr.i * C::kTile;
-        if (flags & TD_FULL) {
-          load_pages<D>(k, &maps.k, k_full + kr.i, row, 0, p.page_rows, go);
-          cp_async_commit();
-        } else {
-          load_slots<D, false>(k, p.k, slots, row, count, 0);
-          cp_async_commit();
-          if (away == 2) landed(false);
-          (away ? away1 : away0) = k_full + kr.i;
-          ++away;
-        }
-        kr.next();
-      }
-      if (away) landed(true);
-      // the loads land before the shared memory goes away, whatever became of their readers
-      mbar_landed_ring(k_full, kr.i, kr.par ^ 1u, NK, status);
-    } else if (warp == 1 || warp == 12) {
-      // ---------------- products of one softmax group ----------------
-      const int w = warp == 12;
+    } else if (warp == 1) {
+      // ---------------- products ----------------
       const uint32_t go = elect_one();
       constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u;
       const uint32_t idesc = (1u << 4) | kType | (8u << 24);
@@ -687,32 +623,28 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       const uint64_t qd0 = tile_desc(smem_u32(sQ), 16, 8 * C::kRow, C::kSwz);
       const uint64_t kd0 = tile_desc(smem_u32(sK), 16, 8 * C::kRow, C::kSwz);
       const uint64_t vd0 = tile_desc(smem_u32(sV), C::kHalf, 8 * C::kRow, C::kSwz);
-      const uint32_t t_s = tmem + C::kS + (uint32_t)(w * 128), t_p = tmem + C::kP + (uint32_t)w * C::kPStep;
-      const uint32_t t_o = tmem + C::kO + (uint32_t)(w * D);
+      const uint32_t t_p = tmem + C::kP, t_o = tmem + C::kO;
       Ring<NK> kr;
-      Ring<NV> vr;
+      Ring<NV> pr;  // of the next product with V
       Ring<ND> dr;
-      uint32_t qpars = 0, jobs = 0;  // query entries' parities, bit e; jobs whose S has been issued
-      int jp = 0;                    // the group that takes the next job
-      bool opened = false;           // this unit's output has a product
-      // the last job, if its product with V is still to come (slots 0: it is not)
-      int p_slots = 0, p_first = 0, p_both = 0, p_vi = 0;
-      uint32_t p_vpar = 0;
-      // the tile in hand: what is waited for next, its description (0), its unit's queries (1), its keys (2), or
-      // nothing any more (3)
-      int need = 0, flags = 0, slots = 0, entry = 0;
-      bool ok = true;
+      Ring<NQ> qr;
+      uint32_t done = 0;             // products with V
+      bool begun = false;            // the last job's product with V is still to come
+      int p_slots = 0, p_first = 0;  // its slots, and whether it opens a unit's output
+      // The tile in hand: what is waited for next, its description (0), its unit's queries (1), its keys (2), or
+      // nothing any more (3).
+      int need = 0, flags = 0, slots = 0, first = 0;
+      int n_slots = 0, n_first = 0;  // of a job whose scores have been issued before the last one's product
 #pragma unroll 1
       while (true) {
-        uint64_t* bar = need == 0 ? d_full + dr.i : need == 1 ? q_full + entry : k_full + kr.i;
-        const uint32_t par = need == 0 ? dr.par : need == 1 ? (qpars >> entry) & 1u : kr.par;
-        // O += P V, before the next scores (they go where the last ones, or P, are), and before waiting for what may
-        // only come after it (a stage of V, the queries' space)
-        if (p_slots && (need >= 2 || !there(bar, par))) {
-          if (!(ok = mbar_wait_ok(p_full + w, (jobs - 1) & 1u, status))) break;
-          if (!(ok = mbar_wait_ok(v_ready + p_vi, p_vpar, status))) break;
+        uint64_t* bar = need == 0 ? d_full + dr.i : need == 1 ? q_full + qr.i : k_full + kr.i;
+        const uint32_t par = need == 0 ? dr.par : need == 1 ? qr.par : kr.par;
+        // O += P V: before the next scores where they, or P, lie in the same columns, after them elsewhere, and
+        // before waiting for what may only come after it (a tile's or the queries' space)
+        if (begun && (n_slots || need == 3 || (!C::kOwnP && need == 2) || !there(bar, par))) {
+          if (!mbar_wait_ok(p_full, done & 1u, status) || !mbar_wait_ok(v_ready + pr.i, pr.par, status)) break;
           tc_fence_after();
-          const uint64_t vd = vd0 + (uint64_t)((p_vi * C::kTile) >> 4);
+          const uint64_t vd = vd0 + (uint64_t)((pr.i * C::kTile) >> 4);
           umma_bf16_tmem_a_if(t_o, t_p, vd, idesc_pv, p_first ? 0u : 1u, go);
           if (p_slots == kSlots) {
 #pragma unroll
@@ -723,75 +655,65 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
             for (int s = 1; s < p_slots; ++s)
               umma_bf16_tmem_a_if(t_o, t_p + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv, 1u, go);
           }
-          umma_commit_if(pv_done + w, go);
-          umma_commit_if(v_empty + p_vi, go);
-          if (!p_both) umma_commit_if(v_empty + p_vi, go);
-          p_slots = 0;
+          umma_commit_if(pv_done, go);
+          umma_commit_if(v_empty + pr.i, go);
+          pr.next();
+          ++done;
+          begun = n_slots != 0;
+          p_slots = n_slots;
+          p_first = n_first;
+          n_slots = 0;
+          continue;
         }
         if (need == 3) break;
-        if (!(ok = mbar_wait_ok(bar, par, status))) break;
+        if (!mbar_wait_ok(bar, par, status)) break;
         if (need == 0) {
           const TileDesc* td = descs + dr.i;
           flags = td->flags;
           slots = td->slots;
-          entry = td->entry;
           if (flags & TD_END) {
             need = 3;
             continue;
           }
           mbar_arrive_lane0(d_empty + dr.i);
           dr.next();
-          need = 2;
-          if (flags & TD_FIRST) {
+          if (flags & TD_FIRST)
             need = 1;
-            continue;
-          }
+          else if (slots)
+            need = 2;
         } else if (need == 1) {
-          qpars ^= 1u << entry;
-          opened = false;
-          need = 2;
+          qr.next();
+          first = 1;
+          need = slots ? 2 : 0;
         } else {
-          // (without columns of its own, P lies where these scores go)
-          if (!C::kOwnP && jobs > 0 && !(ok = mbar_wait_ok(pv_done + w, (jobs - 1) & 1u, status))) break;
+          // (S is free when its weights are there; without columns of its own, P lies there until its product is done)
+          if (begun && !mbar_wait_ok(p_full, done & 1u, status)) break;
+          if (!C::kOwnP && done > 0 && !mbar_wait_ok(pv_done, (done - 1) & 1u, status)) break;
           tc_fence_after();
-          const bool both = flags & TD_BOTH;
-          const uint64_t qd = qd0 + (uint64_t)(((both ? w : entry) * C::kTile) >> 4);
-          const uint64_t kd = kd0 + (uint64_t)((kr.i * C::kTile) >> 4);
+          const int qi = qr.i == 0 ? NQ - 1 : qr.i - 1;
+          const uint64_t qd = qd0 + (uint64_t)((qi * C::kTile) >> 4), kd = kd0 + (uint64_t)((kr.i * C::kTile) >> 4);
           const uint32_t id = idesc | ((uint32_t)(slots * 2) << 17);
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             const uint64_t at = (uint64_t)(((kk * 32) / C::kRow * C::kHalf + (kk * 32) % C::kRow) >> 4);
-            umma_bf16_if(t_s, qd + at, kd + at, id, kk != 0 ? 1u : 0u, go);
+            umma_bf16_if(tmem, qd + at, kd + at, id, kk != 0 ? 1u : 0u, go);
           }
-          umma_commit_if(s_full + w, go);
+          umma_commit_if(s_full, go);
           umma_commit_if(k_empty + kr.i, go);
-          if (!both) umma_commit_if(k_empty + kr.i, go);
-          ++jobs;
-          p_slots = slots;
-          p_first = !opened;
-          p_both = both;
-          p_vi = vr.i;
-          p_vpar = vr.par;
-          opened = true;
           kr.next();
-          vr.next();
-          need = 0;
-          continue;
-        }
-        // a tile without keys, or the other group's, is passed over
-        if (slots == 0) {
-          need = 0;
-        } else if (!(flags & TD_BOTH)) {
-          const bool mine = jp == w;
-          jp ^= 1;
-          if (!mine) {
-            kr.next();
-            vr.next();
-            need = 0;
+          if (begun) {
+            n_slots = slots;
+            n_first = first;
+          } else {
+            begun = true;
+            p_slots = slots;
+            p_first = first;
           }
+          first = 0;
+          need = 0;
         }
       }
-      umma_drain(drain + w, status, go);
+      umma_drain(drain, status, go);
     } else if (warp == 2) {
       // ---------------- values ----------------
       // A tile is loaded, and the one before it then made ready (or at once, while the next has to wait).
@@ -913,112 +835,131 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
       cp_async_wait();
       if (!ok && pending && (last.flags & TD_FULL)) mbar_landed(v_full + last.stage, (full >> last.stage) & 1u, status);
       if (!ok && issued && (next.flags & TD_FULL)) mbar_landed(v_full + next.stage, (full >> next.stage) & 1u, status);
-    } else if (warp == 3) {
-      // ---------------- queries ----------------
-      Ring<2> ur;
-      uint32_t uses[2] = {0, 0};
+    } else {
+      // ---------------- queries and keys ----------------
+      const uint32_t go = elect_one();
+      Ring<NK> kr;
+      Ring<ND> dr;
+      Ring<NQ> qr;
+      uint32_t unit = 0;
+      // Slots on their way by cp.async, oldest first: their tiles are announced once they have landed, at the latest
+      // before this warp waits for anything.
+      int away = 0;
+      uint64_t *away0 = nullptr, *away1 = nullptr;
+      auto landed = [&](bool all) {
+        if (all)
+          cp_async_wait_group<0>();
+        else
+          cp_async_wait_group<2>();
+        fence_async_shared();
+        mbar_arrive_lane0(away0);
+        if (all && away == 2) mbar_arrive_lane0(away1);
+        away0 = away1;
+        away = all ? 0 : away - 1;
+      };
+      auto wait = [&](uint64_t* bar, uint32_t par) {
+        if (away && !there(bar, par)) landed(true);
+        return mbar_wait_ok(bar, par, status);
+      };
       while (true) {
-        if (!mbar_wait_ok(u_full + ur.i, ur.par, status)) break;
-        const UnitInfo u = units[ur.i];
-        if (u.end) break;
-        const int e = ur.i;
-        const uint32_t ur_par = ur.par;
-        mbar_arrive_lane0(u_empty + e);
-        ur.next();
-        // what the rows see, sequence by sequence (before their queries' space is free)
-        bool ok = mbar_wait_ok(r_free + e, ur_par ^ 1u, status);
-        if (!ok) break;
-        const int t_first = u.r0 / p.hr, h_first = u.r0 - t_first * p.hr;  // the unit's first row: token, query head
-        auto at = [&](int r, int& t, int& h) {  // (a product instead of a division: exact below 2^16)
-          const int q = (int)__umulhi((uint32_t)(h_first + r), (uint32_t)p.hr_inv);
-          t = u.t0 + t_first + (p.hr == 1 ? r : q);
-          h = u.head * p.hr + (p.hr == 1 ? 0 : h_first + r - q * p.hr);
-        };
-        {
-          RowInfo* info = rinfo + e * 256;
-          int2 k[8];
+        if (!wait(d_full + dr.i, dr.par)) break;
+        const TileDesc* td = descs + dr.i;
+        const int flags = td->flags, slots = td->slots, row = td->row[lane & (kSlots - 1)], count = td->count[lane & (kSlots - 1)];
+        if (flags & TD_END) break;
+        const UnitInfo u = units[unit % kUnitsAhead];
+        mbar_arrive_lane0(d_empty + dr.i);
+        dr.next();
+        if (flags & TD_FIRST) {
+          const int t_first = u.r0 / p.hr, h_first = u.r0 - t_first * p.hr;  // the unit's first row: token, query head
+          auto at = [&](int r, int& t, int& h) {  // (a product instead of a division: exact below 2^16)
+            const int q = (int)__umulhi((uint32_t)(h_first + r), (uint32_t)p.hr_inv);
+            t = u.t0 + t_first + (p.hr == 1 ? r : q);
+            h = u.head * p.hr + (p.hr == 1 ? 0 : h_first + r - q * p.hr);
+          };
+          int2 k[4];  // what the rows see
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
+          for (int i = 0; i < 4; ++i) {
             int t, h;
             at(lane + 32 * i, t, h);
             k[i] = lane + 32 * i < u.rows ? __ldg(p.tok + t) : make_int2(-5, 0);
           }
+          if (!wait(q_free + qr.i, qr.par ^ 1u)) break;
+          // the queries: pieces of 16 bytes, swizzled as TMA would have it
+          constexpr int NP = D / 8, RP = 32 / NP;  // pieces of a row, rows of a step
+          const int pc = lane % NP;
+          const uint32_t to = smem_u32(sQ) + qr.i * C::kTile + (uint32_t)(pc * 16) / C::kRow * C::kHalf;
+          const uint32_t poff = (uint32_t)(pc * 16) % C::kRow;
+#pragma unroll 4
+          for (int r = lane / NP; r < u.rows; r += RP) {
+            int t, h;
+            at(r, t, h);
+            const uint32_t mask = C::kRow == 128 ? ((uint32_t)r & 7u) : (((uint32_t)r >> 1) & 3u);
+            cp_async16(to + (uint32_t)r * C::kRow + (poff ^ (mask << 4)),
+                       reinterpret_cast<const T*>(p.q) + (long long)t * p.q_row + h * p.q_head + pc * 8);
+          }
+          RowInfo* info = rinfo + qr.i * 128;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
+          for (int i = 0; i < 4; ++i) {
             int t, h;
             at(lane + 32 * i, t, h);
             info[lane + 32 * i] = RowInfo{k[i].x, k[i].y, k[i].x < 0 ? -1 : t * p.hq + h, 0};
           }
+          // (announced as a tile's slots are)
+          cp_async_commit();
+          if (away == 2) landed(false);
+          (away ? away1 : away0) = q_full + qr.i;
+          ++away;
+          qr.next();
         }
-        const int h0 = u.both ? 0 : e, h1 = u.both ? 1 : e;
-        for (int h = h0; h <= h1 && ok; ++h) {
-          if (uses[h] > 0) ok = mbar_wait_ok(q_free + h, (uses[h] - 1) & 1u, status);
-          ++uses[h];
+        if (flags & TD_LAST) ++unit;
+        if (slots == 0) continue;
+        if (!wait(k_empty + kr.i, kr.par ^ 1u)) break;
+        uint8_t* k = sK + kr.i * C::kTile;
+        if (flags & TD_FULL) {
+          load_pages<D>(k, &maps.k, k_full + kr.i, row, 0, p.page_rows, go);
+          cp_async_commit();
+        } else {
+          load_slots<D, false>(k, p.k, slots, row, count, 0);
+          cp_async_commit();
+          if (away == 2) landed(false);
+          (away ? away1 : away0) = k_full + kr.i;
+          ++away;
         }
-        if (!ok) break;
-        // the queries: pieces of 16 bytes, swizzled as TMA would have it
-        constexpr int NP = D / 8, RP = 32 / NP;  // pieces of a row, rows of a step
-        const int pc = lane % NP;
-        const uint32_t hoff = (uint32_t)(pc * 16) / C::kRow * C::kHalf, poff = (uint32_t)(pc * 16) % C::kRow;
-#pragma unroll 4
-        for (int r = lane / NP; r < u.rows; r += RP) {
-          int t, h;
-          at(r, t, h);
-          const T* src = reinterpret_cast<const T*>(p.q) + (long long)t * p.q_row + h * p.q_head + pc * 8;
-          const uint32_t row = (uint32_t)(r & 127);
-          const uint32_t mask = C::kRow == 128 ? (row & 7u) : ((row >> 1) & 3u);
-          cp_async16(smem_u32(sQ) + (uint32_t)((u.both ? r >> 7 : e) * C::kTile) + hoff + row * C::kRow + (poff ^ (mask << 4)), src);
-        }
-        cp_async_wait();
-        fence_async_shared();
-        mbar_arrive_lane0(q_full + e);
+        kr.next();
       }
+      if (away) landed(true);
       cp_async_wait();
+      // the loads land before the shared memory goes away, whatever became of their readers
+      mbar_landed_ring(k_full, kr.i, kr.par ^ 1u, NK, status);
     }
   } else {
     // ---------------- softmax and output ----------------
-    const int w = (warp - 4) >> 2, qd = warp & 3, row = qd * 32 + lane;
-    const uint32_t tl = tmem + ((uint32_t)(qd * 32) << 16);
-    const uint32_t t_s = tl + C::kS + (uint32_t)(w * 128), t_p = tl + C::kP + (uint32_t)w * C::kPStep;
-    const uint32_t t_o = tl + C::kO + (uint32_t)(w * D);
+    const int row = threadIdx.x & 127;
+    const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = tl, t_p = tl + C::kP, t_o = tl + C::kO;
     const float sc = p.sc;
     Ring<ND> dr;
-    uint32_t qpars = 0, jobs0 = 0, jobs1 = 0;  // query entries' parities, bit e; the groups' jobs so far
-    uint32_t joined = 0;                       // units that both groups had a part in
-    bool partner = false;                      // the other group may still be reading this one's output of the last unit
-    int jp = 0, mine0 = 0, mine1 = 0;          // the group that takes the next job; their jobs of this unit
-    uint32_t unit = 0;
+    Ring<NQ> qr;
+    uint32_t jobs = 0, unit = 0;
+    int mine = 0;  // jobs of this unit
     RowInfo ri = {-5, 0, -1, 0};
     float m = -INFINITY, l = 0.f;
     bool spoiled = false, active = false;
     while (true) {
       if (!mbar_wait_ok(d_full + dr.i, dr.par, status)) break;
       const TileDesc* td = descs + dr.i;
-      const int flags = td->flags, slots = td->slots;
+      const int flags = td->flags, slots = td->slots, piece = td->piece;
       if (flags & TD_END) break;
-      const bool both = flags & TD_BOTH;
-      const int entry = td->entry, piece = td->piece;
       if (flags & TD_FIRST) {
-        if (!mbar_wait_ok(q_full + entry, (qpars >> entry) & 1u, status)) break;
-        qpars ^= 1u << entry;
-        if (partner && !mbar_wait_ok(x_read + (1 - w) * 4 + qd, (joined - 1) & 1u, status)) break;
-        partner = false;
-        ri = rinfo[entry * 256 + (both ? w * 128 : 0) + row];
-        mbar_arrive_lane0(r_free + entry);
+        if (!mbar_wait_ok(q_full + qr.i, qr.par, status)) break;
+        ri = rinfo[qr.i * 128 + row];
         active = __any_sync(0xffffffffu, ri.seq >= 0);
         m = -INFINITY;
         l = 0.f;
-        mine0 = mine1 = 0;
+        mine = 0;
         spoiled = ri.seen < 0;
       }
-      const bool job0 = slots > 0 && (both || jp == 0), job1 = slots > 0 && (both || jp == 1);
-      if (slots > 0 && !both) jp ^= 1;
-      const uint32_t jobs = w ? jobs1 : jobs0;
-      const int mine = w ? mine1 : mine0;
-      jobs0 += job0, jobs1 += job1;
-      mine0 += job0, mine1 += job1;
-      if (w ? job1 : job0) {
-        if (!mbar_wait_ok(s_full + w, jobs & 1u, status)) break;
+      if (slots > 0) {
+        if (!mbar_wait_ok(s_full, jobs & 1u, status)) break;
         if (active) {
           tc_fence_after();
           // Scores are read twice, for the maximum and for P, and never held (code and registers: the roles'
@@ -1107,8 +1048,8 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           } else {
             const bool up = mx > m + kSlack;
             if (__any_sync(0xffffffffu, up)) {
-              // the accumulator, complete up to this group's last job, to the new maximum
-              if (!mbar_wait_ok(pv_done + w, (jobs - 1) & 1u, status)) break;
+              // the accumulator, complete up to the last job, to the new maximum
+              if (!mbar_wait_ok(pv_done, (jobs - 1) & 1u, status)) break;
               tc_fence_after();
               const float f = up ? ex2_approx(m - mx) : 1.f;
               if (up) m = mx;
@@ -1124,7 +1065,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
             }
           }
           if (C::kOwnP && jobs > 0) {  // P's columns are free once the last job's product has read them
-            if (!mbar_wait_ok(pv_done + w, (jobs - 1) & 1u, status)) break;
+            if (!mbar_wait_ok(pv_done, (jobs - 1) & 1u, status)) break;
             tc_fence_after();
           }
           const float ref = m == -INFINITY ? 0.f : m;
@@ -1192,13 +1133,18 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
           tmem_st_wait();
           tc_fence_before();
         }
-        mbar_arrive_lane0(p_full + w);
+        mbar_arrive_lane0(p_full);
+        ++jobs;
+        ++mine;
       }
       mbar_arrive_lane0(d_empty + dr.i);
       dr.next();
       if (!(flags & TD_LAST)) continue;
 
       // ---------------- the piece's output ----------------
+      // (every S of the unit is complete: its queries may go)
+      mbar_arrive_lane0(q_free + qr.i);
+      qr.next();
       if (!mbar_wait_ok(cleaned + unit % kUnitsAhead, (unit / kUnitsAhead) & 1u, status)) break;
       {
         const Dirty dt = dirty[unit % kUnitsAhead];
@@ -1210,89 +1156,50 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 1)
         ++unit;
       }
       if (spoiled) l = NAN;
-      // every S of this group is complete: the unit's queries may go
-      if (both) {
-        mbar_arrive_lane0(q_free);
-        mbar_arrive_lane0(q_free + 1);
-      } else {
-        mbar_arrive_lane0(q_free + entry);
-      }
-      // Each group reads its own rows' output, or, of rows that both had a part in, half of the columns of both
-      // outputs (a warp's TMEM lanes are its partner's).
-      bool have0 = both ? mine > 0 || (w ? job1 : job0) : mine0 > 0, have1 = !both && mine1 > 0;
-      float f0 = 1.f, f1 = 0.f, ms = m, ls = l;
-      if (!both) {
-        s_ml[w * 128 + row] = make_float2(m, l);
-        mbar_arrive_lane0(x_full + w * 4 + qd);
-        if (!mbar_wait_ok(x_full + (1 - w) * 4 + qd, joined & 1u, status)) break;
-        ++joined;
-        partner = true;
-        const float2 a = s_ml[row], b = s_ml[128 + row];
-        ms = fmaxf(a.x, b.x);
-        const float ref = ms == -INFINITY ? 0.f : ms;
-        f0 = ex2_approx(a.x - ref);
-        f1 = ex2_approx(b.x - ref);
-        ls = fmaf(a.y, f0, b.y * f1);
-      }
-      const bool store = ri.out >= 0;
-      if (piece < 0) {
-        const float inv = ls == 0.f ? 0.f : 1.f / ls;
-        f0 *= inv;
-        f1 *= inv;
-      }
-      if (have0 && !mbar_wait_ok(pv_done + (both ? w : 0), ((both && w ? jobs1 : jobs0) - 1) & 1u, status)) break;
-      if (have1 && !mbar_wait_ok(pv_done + 1, (jobs1 - 1) & 1u, status)) break;
-      tc_fence_after();
-      const long long slot = ((long long)blockIdx.x * 2 + (piece == 1)) * kUnitRows + (both ? w * 128 : 0) + row;
+      const bool store = ri.out >= 0, direct = piece < 0;
+      const float f = !direct ? 1.f : l == 0.f ? 0.f : 1.f / l;
+      const long long slot = ((long long)blockIdx.x * 2 + (piece == 1)) * kUnitRows + row;
       T* out = reinterpret_cast<T*>(p.out) + (long long)ri.out * D;
       float* part = p.part_o + slot * D;
-      const uint32_t t_o0 = both ? t_o : tl + C::kO, t_o1 = tl + C::kO + (uint32_t)D;
-      const int c_end = both ? D : (w + 1) * (D / 2);
+      if (mine > 0) {
+        if (!mbar_wait_ok(pv_done, (jobs - 1) & 1u, status)) break;
+        tc_fence_after();
+      }
 #pragma unroll 1
-      for (int c0 = both ? 0 : w * (D / 2); c0 < c_end; c0 += 16) {
-        float o[16], o1[16];
-        if (have0) {
-          tmem_ld16(t_o0 + (uint32_t)c0, o);
+      for (int c0 = 0; c0 < D; c0 += 32) {
+        float o[32];
+        if (mine > 0) {
+          tmem_ld32(t_o + (uint32_t)c0, o);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[i] *= f0;
+          for (int i = 0; i < 32; ++i) o[i] *= f;
         } else {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[i] = 0.f;
+          for (int i = 0; i < 32; ++i) o[i] = 0.f;
         }
-        if (have1) {
-          tmem_ld16(t_o1 + (uint32_t)c0, o1);
+        if (store && direct) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o[i] = fmaf(o1[i], f1, o[i]);
-        }
-        if (store) {
-          if (piece < 0) {
-            *reinterpret_cast<uint4*>(out + c0) = piece_put<T>(o);
-            *reinterpret_cast<uint4*>(out + c0 + 8) = piece_put<T>(o + 8);
-          } else {
-            st_sector(part + c0, o);
-            st_sector(part + c0 + 8, o + 8);
-          }
+          for (int i = 0; i < 32; i += 8) *reinterpret_cast<uint4*>(out + c0 + i) = piece_put<T>(o + i);
+        } else if (store) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) st_sector(part + c0 + i, o + i);
         }
       }
       tc_fence_before();
-      if (!both) mbar_arrive_lane0(x_read + w * 4 + qd);
-      if (store && (both || w == 0)) {
-        if (piece < 0) {
-          if (!(ls == ls)) {
-            const int at = atomicAdd(&p.head->listed, 1);
-            if (at < kListed) p.list[at] = ri.out;
-          }
-          if (p.lse) p.lse[ri.out] = ls == 0.f ? -INFINITY : (ms + log2f(ls)) * 0.693147180559945309f;
-        } else {
-          p.part_ml[slot] = make_float2(ms, ls);
+      if (store && direct) {
+        if (!(l == l)) {
+          const int at = atomicAdd(&p.head->listed, 1);
+          if (at < kListed) p.list[at] = ri.out;
         }
+        if (p.lse) p.lse[ri.out] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
+      } else if (store) {
+        p.part_ml[slot] = make_float2(m, l);
       }
     }
   }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == 1) tmem_dealloc(tmem, 512);
+  if (warp == 1) tmem_dealloc(tmem, C::kCols);
 }
 
 // ---------------------------------------------------------------------------
@@ -1527,7 +1434,7 @@ cudaError_t prefix_go(const PageMaps& m, const PrefixParams& p, cudaStream_t s) 
   cudaError_t e = launch_k(prefix_plan_kernel, dim3(kPlanCtas), dim3(kPlanThreads), 0, s, p);
   if (e == cudaSuccess)
     e = launch_k(prefix_attend_kernel<T, D>, dim3((unsigned)p.ctas), dim3(C::kThreads), C::kSmem, s, m, p);
-  if (e == cudaSuccess) e = launch_k(prefix_finish_kernel<T, D>, dim3((unsigned)p.ctas, 8), dim3(256), 0, s, p);
+  if (e == cudaSuccess) e = launch_k(prefix_finish_kernel<T, D>, dim3((unsigned)p.ctas, 4), dim3(256), 0, s, p);
   return e;
 }
 template <typename T>
@@ -1546,7 +1453,7 @@ extern "C" uint64_t fe_prefix_attention_workspace(const fe_prefix_args* a) {
     fail_cuda(dev.err, "fe_prefix_attention_workspace");
     return 0;
   }
-  return layout(a, dev.sms, most_tiles(a)).bytes;
+  return layout(a, 2 * dev.sms, most_tiles(a)).bytes;
 }
 
 extern "C" int fe_prefix_attention(const fe_prefix_args* a, void* stream) {
@@ -1558,7 +1465,7 @@ extern "C" int fe_prefix_attention(const fe_prefix_args* a, void* stream) {
   const Device& dev = device();
   if (dev.err != cudaSuccess) return fail_cuda(dev.err, "fe_prefix_attention");
   PrefixParams p{};
-  p.ctas = dev.sms;
+  p.ctas = 2 * dev.sms;
   p.max_tiles = most_tiles(a);
   const Layout w = layout(a, p.ctas, p.max_tiles);
   if (a->workspace_bytes < w.bytes) return fail(FE_ERR_WORKSPACE, "workspace too small");
