@@ -975,6 +975,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
           auto pair = [&](int z, float* v) {  // scores of slots 2 z and 2 z + 1, unseen ones -inf
             tmem_ld32(t_s + (uint32_t)(32 * z), v);
             const uint32_t two = (z < 2 ? seen0 : seen1) >> (16 * (z & 1));
+            if (__all_sync(0xffffffffu, (two & 0xffffu) == 0x1010u)) return;
             const int n0 = two & 0xff, n1 = (two >> 8) & 0xff;
 #pragma unroll
             for (int i = 0; i < kSlot; ++i) {
@@ -1207,7 +1208,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
 // ---------------------------------------------------------------------------
 // A row from its visible keys alone, 32 at a time, by one warp (sq: its D queries)
 template <typename T, int D>
-__device__ void row_by_keys(const PrefixParams& p, long long w, float* sq) {
+__device__ __noinline__ void row_by_keys(const PrefixParams& p, long long w, float* sq) {
   const int lane = threadIdx.x & 31;
   const int t = (int)(w / p.hq), h = (int)(w % p.hq), hk = h / (p.hq / p.hkv);
   const int s = warp_find_row(p.row_start, p.n_seqs, t), g = warp_find_row(p.group_start, p.n_groups, s);
@@ -1293,6 +1294,12 @@ __global__ void __launch_bounds__(256) prefix_finish_kernel(const PrefixParams p
   const SplitRec rec = p.recs[blockIdx.x];
   if (rec.pieces > 0) {
     constexpr int N = D / 32;
+    struct alignas(4 * N) Values {
+      float v[N];
+    };
+    struct alignas(2 * N) Outputs {
+      T v[N];
+    };
     const long long first = (long long)blockIdx.x * 2 + 1;
     auto slot = [&](int i, int r) { return (i == 0 ? first : 2LL * (blockIdx.x + i)) * kUnitRows + r; };
     for (int r = blockIdx.y * 8 + wp; r < rec.rows; r += gridDim.y * 8) {
@@ -1302,11 +1309,11 @@ __global__ void __launch_bounds__(256) prefix_finish_kernel(const PrefixParams p
       float l = 0.f, o[N] = {};
       for (int i = 0; i <= rec.pieces; ++i) {
         const float2 ml = p.part_ml[slot(i, r)];
+        const Values x = reinterpret_cast<const Values*>(p.part_o + slot(i, r) * D)[lane];
         const float f = ex2_approx(ml.x - ref);
         l = fmaf(ml.y, f, l);
-        const float* po = p.part_o + slot(i, r) * D + lane * N;
 #pragma unroll
-        for (int z = 0; z < N; ++z) o[z] = fmaf(po[z], f, o[z]);
+        for (int z = 0; z < N; ++z) o[z] = fmaf(x.v[z], f, o[z]);
       }
       const int rr = rec.r0 + r;
       const long long w = (long long)(rec.t0 + rr / p.hr) * p.hq + rec.head * p.hr + rr % p.hr;
@@ -1317,9 +1324,10 @@ __global__ void __launch_bounds__(256) prefix_finish_kernel(const PrefixParams p
         row_by_keys<T, D>(p, w, sq[wp]);
         continue;
       }
-      T* out = reinterpret_cast<T*>(p.out) + w * D + lane * N;
+      Outputs y;
 #pragma unroll
-      for (int z = 0; z < N; ++z) out[z] = Elem<T>::put(o[z]);
+      for (int z = 0; z < N; ++z) y.v[z] = Elem<T>::put(o[z]);
+      reinterpret_cast<Outputs*>(reinterpret_cast<T*>(p.out) + w * D)[lane] = y;
       if (p.lse && lane == 0) p.lse[w] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
     }
   }
