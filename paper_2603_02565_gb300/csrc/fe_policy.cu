@@ -9,16 +9,19 @@
 //
 // Bound by memory: at least each logit is read once and its gradient written once.  A row's
 // gradient needs the whole row's sum first, so it stays on the SM in between where it fits:
-//   rows up to 16 KB   in the registers of a CTA of 128 threads, eight CTAs an SM
-//   longer rows        the first pass keeps 64 KB of the row (52 KB in rows up to 64 KB) in
-//                      shared memory and asks L2 to hold the rest, which the second pass
-//                      reads again; gradients leave with the lowest claim on L2.
+//   rows up to 64 KB   in the registers of a CTA, whose threads (32 to 512) hold up to eight
+//                      pieces of 16 bytes each: 1024 threads an SM, in as many CTAs as they make
+//   longer rows        the first pass keeps 64 KB of the row in shared memory and asks L2 to
+//                      hold the rest, which the second pass reads again; gradients leave with
+//                      the lowest claim on L2.  Few rows: up to eight CTAs share one.
 // What matters is rows in different phases beside one another: three CTAs of 512 threads an SM
-// (four of 256 for rows up to 64 KB).  4096 tokens x 100000 words in bf16 (241 us at the copy
+// for long rows.  4096 tokens x 100000 words in bf16 (241 us at the copy
 // rate): 295 us; without the L2 hints 315, everything read twice 397 (hints alone 313), two
 // CTAs 322, one of 1024 threads 345.  A ring of bulk copies several rows deep in one CTA of
 // 512 threads took 440: its phases do not overlap, and clusters that share a row pay several
-// us a row (710 with the row in the registers of four CTAs).  16384 x 8192 (79 us): 96 us.
+// us a row (710 with the row in the registers of four CTAs).  In registers, 16384 tokens in bf16:
+// x 1000 (10 us) 21 us (28 with 128 threads, where most have nothing to do), x 8192 (79) 96,
+// x 16000 (154) 171 and x 32000 (309) 342 (213 and 381 by way of shared memory).
 #include <algorithm>
 #include <cmath>
 #include <mutex>
@@ -134,7 +137,10 @@ struct RowSplit {
 
 template <int THREADS, typename T>
 __device__ __forceinline__ void zero_row(T* g, int n) {
-  for (int i = threadIdx.x; i < n; i += THREADS) g[i] = Elem<T>::put(0.f);
+  const RowSplit<T> rs(g, n);
+  if ((int)threadIdx.x < rs.head) g[threadIdx.x] = Elem<T>::put(0.f);
+  for (int i = threadIdx.x; i < rs.pieces; i += THREADS) reinterpret_cast<uint4*>(g + rs.head)[i] = make_uint4(0u, 0u, 0u, 0u);
+  for (int i = rs.head + rs.pieces * Elem<T>::N + threadIdx.x; i < n; i += THREADS) g[i] = Elem<T>::put(0.f);
 }
 
 // grad = k (1[v = y] - 2^((x - b) c) / sum) over a row
@@ -250,13 +256,12 @@ __device__ __forceinline__ int edge_of(int i, const RowSplit<T>& rs, int n) {
   return i < 2 * N && at < n ? at : -1;
 }
 
-// Rows up to 16 KB: a CTA of 128 threads holds one in registers between its statistics and its gradient; eight
-// CTAs an SM keep loads in flight while others compute.
-constexpr int kRowThreads = 128;
-template <typename T, int NV>
-__global__ void __launch_bounds__(kRowThreads, 8) policy_row_kernel(const PolicyParams p) {
+// A CTA holds a row in registers between its statistics and its gradient; with 1024 threads an SM (64 registers
+// each) loads are in flight while other rows compute.
+template <typename T, int THREADS, int NV>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) policy_row_kernel(const PolicyParams p) {
   constexpr int N = Elem<T>::N;
-  __shared__ MaxSum sh[kRowThreads / 32];
+  __shared__ MaxSum sh[THREADS / 32];
   __shared__ float s_k;
   pdl_trigger();
   pdl_wait();
@@ -266,7 +271,7 @@ __global__ void __launch_bounds__(kRowThreads, 8) policy_row_kernel(const Policy
   T* g = p.grad ? reinterpret_cast<T*>(p.grad) + (long long)t * p.grad_row : nullptr;
   if (!k.kept()) {
     if (threadIdx.x == 0) p.terms[t] = p.logp[t] = p.lse[t] = p.coef[t] = 0.f;
-    if (g) zero_row<kRowThreads>(g, p.vocab);
+    if (g) zero_row<THREADS>(g, p.vocab);
     return;
   }
   const RowSplit<T> rs(x, p.vocab);
@@ -275,7 +280,7 @@ __global__ void __launch_bounds__(kRowThreads, 8) policy_row_kernel(const Policy
   uint4 w[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int at = threadIdx.x + i * kRowThreads;
+    const int at = threadIdx.x + i * THREADS;
     if (at < rs.pieces) w[i] = ld_stream(xi + at * N);
   }
   const float ze = edge >= 0 ? Elem<T>::get(x[edge]) : -INFINITY;
@@ -284,17 +289,17 @@ __global__ void __launch_bounds__(kRowThreads, 8) policy_row_kernel(const Policy
   MaxSum v = {ze, 0.f};
 #pragma unroll
   for (int i = 0; i < NV; ++i)
-    if (threadIdx.x + i * kRowThreads < rs.pieces) v.m = piece_max<T>(w[i], v.m);
+    if (threadIdx.x + i * THREADS < rs.pieces) v.m = piece_max<T>(w[i], v.m);
   const uint64_t c2 = f32x2_pack(p.c, p.c);
   {
     const uint64_t nb = f32x2_pack(-base_of(v.m), -base_of(v.m));
     uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-      if (threadIdx.x + i * kRowThreads < rs.pieces) piece_sum<T>(w[i], nb, c2, sum);
+      if (threadIdx.x + i * THREADS < rs.pieces) piece_sum<T>(w[i], nb, c2, sum);
     v.s = sum_of(sum) + ex2_approx((ze - base_of(v.m)) * p.c);
   }
-  v = block_join<kRowThreads>(v, p.c, sh);
+  v = block_join<THREADS>(v, p.c, sh);
   if (threadIdx.x == 0) s_k = row_outputs(p, t, k, xy, v, true);
   if (!g) return;
   __syncthreads();
@@ -303,7 +308,7 @@ __global__ void __launch_bounds__(kRowThreads, 8) policy_row_kernel(const Policy
   T* gi = g + rs.head;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int at = threadIdx.x + i * kRowThreads;
+    const int at = threadIdx.x + i * THREADS;
     if (at < rs.pieces) *reinterpret_cast<uint4*>(gi + at * N) = piece_grad<T>(w[i], nb, c2, f, kf, k.y - rs.head - at * N);
   }
   if (edge >= 0) g[edge] = Elem<T>::put(fmaf(f, ex2_approx((ze - b) * p.c), edge == k.y ? kf : 0.f));
@@ -452,21 +457,38 @@ __global__ void __launch_bounds__(kThreads) policy_backward_kernel(const PolicyP
 }
 
 // loss = sum of the terms: each thread its own in turn, then a tree, in 64 bits
-__global__ void __launch_bounds__(1024) policy_sum_kernel(const float* terms, int rows, float* loss) {
-  __shared__ double sh[32];
+// (fp64 additions are slow here, half a microsecond for a thousand: many rows are spread over a cluster's SMs, 5 us
+// for 16384 terms where one CTA of 1024 threads took 13: its shuffles alone add 5000 times)
+constexpr int kSumThreads = 256, kSumCtas = 8;
+__global__ void __launch_bounds__(kSumThreads) policy_sum_kernel(const float* terms, int rows, float* loss) {
+  constexpr int W = kSumThreads / 32;
+  __shared__ double sh[W], s_parts[kSumCtas];
   pdl_trigger();
+  cluster_arrive();
   pdl_wait();
+  const int rank = blockIdx.x, step = gridDim.x * kSumThreads;
   double s = 0.0;
-  for (int i = threadIdx.x; i < rows; i += 1024) s += (double)terms[i];
+#pragma unroll 8
+  for (int i = rank * kSumThreads + threadIdx.x; i < rows; i += step) s += (double)terms[i];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
   __syncthreads();
-  if (threadIdx.x < 32) {
-    s = sh[threadIdx.x];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (threadIdx.x == 0) *loss = (float)s;
+  cluster_wait();  // (every CTA has begun)
+  if (threadIdx.x == 0) {
+    s = sh[0];
+    for (int i = 1; i < W; ++i) s += sh[i];
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(smem_u32(s_parts + rank)));
+    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(at), "d"(s) : "memory");
+  }
+  __syncwarp();
+  cluster_arrive();
+  cluster_wait();
+  if (rank == 0 && threadIdx.x == 0) {
+    s = s_parts[0];
+    for (int i = 1; i < (int)gridDim.x; ++i) s += s_parts[i];
+    *loss = (float)s;
   }
 }
 
@@ -508,12 +530,16 @@ cudaError_t policy_go(const PolicyParams& p, cudaStream_t s) {
   const int pieces = (p.vocab + N - 1) / N;
   // a gradient whose rows start elsewhere between two 16-byte boundaries cannot leave in 16-byte pieces
   const bool aligned = !p.grad || ((((uintptr_t)p.grad ^ (uintptr_t)p.logits) & 15) == 0 && (p.grad_row - p.logits_row) % N == 0);
-  if (aligned && pieces <= kRowThreads * 8) {
-    const dim3 g((unsigned)p.rows), b(kRowThreads);
-    if (pieces <= kRowThreads) return launch_k(policy_row_kernel<T, 1>, g, b, 0, s, p);
-    if (pieces <= kRowThreads * 2) return launch_k(policy_row_kernel<T, 2>, g, b, 0, s, p);
-    if (pieces <= kRowThreads * 4) return launch_k(policy_row_kernel<T, 4>, g, b, 0, s, p);
-    return launch_k(policy_row_kernel<T, 8>, g, b, 0, s, p);
+  if (aligned && pieces <= 4096) {
+    const dim3 g((unsigned)p.rows);
+    if (pieces <= 128) return launch_k(policy_row_kernel<T, 32, 4>, g, dim3(32), 0, s, p);
+    if (pieces <= 256) return launch_k(policy_row_kernel<T, 64, 4>, g, dim3(64), 0, s, p);
+    if (pieces <= 512) return launch_k(policy_row_kernel<T, 128, 4>, g, dim3(128), 0, s, p);
+    if (pieces <= 1024) return launch_k(policy_row_kernel<T, 128, 8>, g, dim3(128), 0, s, p);
+    if (pieces <= 1536) return launch_k(policy_row_kernel<T, 256, 6>, g, dim3(256), 0, s, p);
+    if (pieces <= 2048) return launch_k(policy_row_kernel<T, 256, 8>, g, dim3(256), 0, s, p);
+    if (pieces <= 3072) return launch_k(policy_row_kernel<T, 512, 6>, g, dim3(512), 0, s, p);
+    return launch_k(policy_row_kernel<T, 512, 8>, g, dim3(512), 0, s, p);
   }
   // few rows: several CTAs each, as long as every thread has a piece
   int cs = 1;
@@ -591,7 +617,9 @@ extern "C" int fe_policy_loss(const fe_policy_args* a, void* stream) {
   cudaError_t e = cudaSuccess;
   if (a->rows > 0)
     e = a->dtype == FE_IO_F32 ? policy_go<float>(p, s) : a->dtype == FE_IO_BF16 ? policy_go<__nv_bfloat16>(p, s) : policy_go<__half>(p, s);
-  if (e == cudaSuccess) e = launch_k(policy_sum_kernel, dim3(1), dim3(1024), 0, s, (const float*)a->terms, a->rows, a->loss);
+  const int cs = a->rows > 8 * kSumThreads ? kSumCtas : 1;
+  if (e == cudaSuccess)
+    e = launch_kc(policy_sum_kernel, dim3((unsigned)cs), dim3(kSumThreads), 0, s, cs, (const float*)a->terms, a->rows, a->loss);
   return e == cudaSuccess ? FE_OK : fail_cuda(e, "fe_policy_loss");
 }
 

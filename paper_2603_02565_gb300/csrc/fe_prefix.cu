@@ -89,6 +89,7 @@ __device__ __forceinline__ int seen_rows(int len, int n, int j) { return max(0, 
 // plan
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024, kPlanGroups = 4096, kPlanCtas = 8;
+static_assert(kPlanThreads == 1024, "block_scan sums the totals of 32 warps");
 
 // inclusive sum over the block's threads
 template <typename V>
