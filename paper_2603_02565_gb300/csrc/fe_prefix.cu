@@ -1360,6 +1360,7 @@ int check_prefix(const fe_prefix_args* a) {
   if (a->n_groups == 0 || a->n_seqs == 0) return fail(FE_ERR_INVALID_ARG, "rows without a sequence or group");
   if (!a->group_start || !a->prefix_len || !a->prefix_pages || !a->row_start || !a->seq_len || !a->pages || !a->q || !a->out)
     return fail(FE_ERR_INVALID_ARG, "null pointer");
+  if (a->out == a->q) return fail(FE_ERR_INVALID_ARG, "out must not be q");
   if (misaligned(a->q, 16) || misaligned(a->out, 16) || a->q_row % 8 != 0 || a->q_head % 8 != 0)
     return fail(FE_ERR_UNSUPPORTED, "rows must be 16-byte aligned, strides multiples of 8");
   return FE_OK;
