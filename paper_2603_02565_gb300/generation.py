@@ -11,7 +11,8 @@ a loss and its gradient to the logits.
 As in `binding`, arguments are checked and passed on: every computation runs in
 the library's kernels, on the current stream unless `stream` (a
 torch.cuda.Stream or its handle) says otherwise.  Nothing waits.  Outputs and
-workspaces that are not passed in are allocated by torch for that stream.  Indices
+workspaces that are not passed in are allocated by torch for that stream; only
+attend's workspace is kept.  Indices
 in device memory are checked by the kernels, which report through `status`, a
 CUDA int32 tensor of one element that the caller zeroes and `check_status` reads.
 """
@@ -19,6 +20,7 @@ from __future__ import annotations
 
 import math
 import struct
+import threading
 
 import torch
 
@@ -62,6 +64,10 @@ def rotary_table(n_positions: int, rot_dim: int, base: float = 10000.0, device="
 
 # the current stream's handle by device index, without a stream object where torch offers that
 _current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+_capturing = torch.cuda.is_current_stream_capturing
+_thread = threading.get_ident
 
 
 def _stream_of(stream, index):
@@ -132,7 +138,8 @@ class PagedKV:
         self._fields = (_TYPES[k.dtype], self.n_pages, self.page_rows, self.kv_heads, self.head_dim, k.data_ptr(),
                         v.data_ptr())
         self._scale = 1.0 / math.sqrt(self.head_dim)
-        self._workspace = {}  # bytes by sizes
+        self._need = {}  # workspace bytes by sizes
+        self._spaces = {}  # a workspace by thread and stream
 
     @classmethod
     def empty(cls, n_pages, page_rows, kv_heads, head_dim, dtype=torch.bfloat16, device="cuda"):
@@ -199,8 +206,8 @@ class PagedKV:
         that sequence s holds in pages[s]; each sees the rows up to itself, and the prefix_lengths[g] rows in
         prefix_pages[g] of the group g with group_start[g] <= s < group_start[g + 1].  scale: 1 / sqrt(head_dim)
         unless given.  Returns out [rows, q_heads, head_dim], with with_lse (out, lse [rows, q_heads] fp32); a
-        row that sees nothing gets 0 and -inf.  workspace: a uint8 tensor to use instead of a fresh one
-        (workspace_bytes says how much); not to be shared by calls that may overlap."""
+        row that sees nothing gets 0 and -inf.  workspace: a uint8 tensor to use instead of the one that this object
+        keeps for each thread and stream (workspace_bytes says how much); not to be shared by calls that may overlap."""
         dev = self._index
         G, S, T = prefix_lengths.shape[0], lengths.shape[0], q.shape[0]
         qp, hq, q_row, q_head = self._rows("q", q, T)
@@ -210,10 +217,17 @@ class PagedKV:
         out = _like(q, on) if out is None else self._out("out", out, q)
         lse = _new(q, (T, hq), on, torch.float32) if with_lse else None
         if workspace is None:
-            need = self._workspace.get((G, S, T, hq))
+            need = self._need.get((G, S, T, hq))
             if need is None:
-                need = self._workspace[G, S, T, hq] = self.workspace_bytes(G, S, T, hq)
-            workspace = _new(q, (need + 1) // 2, on)
+                need = self._need[G, S, T, hq] = self.workspace_bytes(G, S, T, hq)
+            # A thread's calls on a stream run one after another and share a workspace (another thread's kernels could
+            # come between the three of a call); a call that is being captured has one of its own, in the graph's memory.
+            key = _thread(), handle
+            workspace = self._spaces.get(key)
+            if workspace is None or workspace.shape[0] < need or _capturing():
+                workspace = _new(q, need, on, torch.uint8)
+                if not _capturing():
+                    self._spaces[key] = workspace
         elif workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be a contiguous uint8 tensor on {self.device}")
         else:
@@ -242,16 +256,15 @@ class PolicyLoss:
     """Outputs of policy_loss: loss (a 0-d tensor), and per token terms (the weighted summands), logp (log
     probability), lse (logsumexp) and coef (the slope of the loss to logp), all fp32; grad [tokens, vocab] or None."""
 
-    __slots__ = ("_stats", "grad")
+    __slots__ = ("_stats", "_tokens", "grad")
 
-    def __init__(self, stats, grad):
-        self._stats, self.grad = stats, grad  # [1 + 4 tokens]: the loss, then the four rows
+    def __init__(self, stats, tokens, grad):
+        self._stats, self._tokens, self.grad = stats, tokens, grad  # [1 + 4 tokens]: the loss, then the four rows
 
     def _row(self, i):
-        n = (self._stats.shape[0] - 1) // 4
-        return self._stats[1 + i * n:1 + (i + 1) * n]
+        return self._stats.narrow(0, 1 + i * self._tokens, self._tokens)
 
-    loss = property(lambda self: self._stats[0])
+    loss = property(lambda self: self._stats.select(0, 0))
     terms = property(lambda self: self._row(0))
     logp = property(lambda self: self._row(1))
     lse = property(lambda self: self._row(2))
@@ -309,7 +322,7 @@ def policy_loss(logits, tokens, advantages, weights=None, *, old_logp=None, ref_
         at + 4 + 3 * n, grad_p, _status(status, dev)), handle)
     if rc:
         _check(rc)
-    return PolicyLoss(stats, grad)
+    return PolicyLoss(stats, T, grad)
 
 
 def policy_loss_backward(logits, tokens, result: PolicyLoss, weights=None, *, upstream=None, temperature=1.0,
