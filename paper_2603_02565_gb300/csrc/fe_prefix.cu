@@ -977,12 +977,10 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
             tmem_ld32(t_s + (uint32_t)(32 * z), v);
             const uint32_t two = (z < 2 ? seen0 : seen1) >> (16 * (z & 1));
             if (__all_sync(0xffffffffu, (two & 0xffffu) == 0x1010u)) return;
-            const int n0 = two & 0xff, n1 = (two >> 8) & 0xff;
+            const uint32_t bits = ((1u << (two & 0xff)) - 1u) | ((1u << ((two >> 8) & 0xff)) - 1u) << kSlot;
 #pragma unroll
-            for (int i = 0; i < kSlot; ++i) {
-              if (i >= n0) v[i] = -INFINITY;
-              if (i >= n1) v[kSlot + i] = -INFINITY;
-            }
+            for (int i = 0; i < 2 * kSlot; ++i)
+              if (!(bits & (1u << i))) v[i] = -INFINITY;
           };
           if (whole) {
 #pragma unroll 1
