@@ -48,9 +48,11 @@ struct PlanHead {
   int listed;   // rows to compute again (more than kListed: all rows are looked at)
   int n_tiles;  // row tiles (units per key head)
 };
-// A split unit, by the CTA that has its first piece: rows and further pieces (0: none)
+// A split unit: its rows, and the CTAs that have its pieces (count 0: none).  While the schedule runs, count is its
+// tiles, the first of them tile.
 struct SplitRec {
-  int pieces, t0, r0, rows, head, pad[3];
+  int first, count, t0, r0, rows, head;
+  long long tile;
 };
 
 struct PrefixParams {
@@ -70,7 +72,7 @@ struct PrefixParams {
   long long* gcost;    // [n_groups + 1] key tiles of all heads before a group
   int* cost;           // [max_tiles] key tiles of a row tile (one head), at least 1
   long long* before;   // [max_tiles + 1] key tiles of one head before a row tile
-  SplitRec* recs;      // [ctas] (two an SM)
+  SplitRec* recs;      // [ctas][2] the split unit that a CTA begins in the middle of, the one it ends in the middle of
   int* list;           // [kListed]
   float* part_o;       // [ctas][2][kUnitRows][D]
   float2* part_ml;     // [ctas][2][kUnitRows] maximum (log2 units) and sum
@@ -445,7 +447,8 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
       long long x = cta < ctas ? begin(cta) : 0;
       Ring<ND> dr;
       bool ok = true;
-      SplitRec rec = {};
+      if (lane < 2) p.recs[2 * cta + lane].count = 0;
+      __syncwarp();
       uint32_t unit = 0;
       // the unit that holds tile x: group, head, row tile; the next ones follow step by step
       int g = 0, head = 0, ti = 0, off = 0, first_rt = 0, n_rt = 0, s0 = 0, s1 = 0, t0 = 0, group_rows = 0, plen = 0;
@@ -474,12 +477,8 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
         const int n = (int)min((long long)(cost - off), hi - x);
         const int r0 = ti * kUnitRows, rows = min(kUnitRows, group_rows - r0);
         const int piece = off == 0 && n == cost ? -1 : off == 0 ? 1 : 0;
-        if (piece == 1) {  // further pieces: the CTAs that begin inside the unit
-          const long long end = x + cost;
-          int c = cta + 1;
-#pragma unroll 1
-          while (c < ctas && begin(c) < end) ++c;
-          rec = SplitRec{c - cta - 1, t0, r0, rows, head, {}};
+        if (piece >= 0) {
+          if (lane == 0) p.recs[2 * cta + piece] = SplitRec{0, cost, t0, r0, rows, head, x - off};
         }
         // (each reader of a unit's entry reads it before it passes on the unit's first tile)
         const UnitInfo info = {t0, r0, rows, head};
@@ -614,7 +613,19 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
         if (lane == 0) descs[dr.i].flags = TD_END;
         mbar_arrive_lane0(d_full + dr.i);
       }
-      if (lane == 0) p.recs[cta] = rec;
+      // (the equal runs are worked out once more: held until here they would cost the loop registers)
+      __syncwarp();
+      SplitRec* rec = p.recs + 2 * cta + (lane & 1);
+      if (lane < 2 && rec->count > 0) {
+        const long long all = p.gcost[p.n_groups], n = min((long long)p.ctas, all), low = all / n, large = all - low * n;
+        auto cta_of = [&](long long tile) {  // that has the tile
+          const long long in_large = (low + 1) * large;
+          return (int)(tile < in_large ? tile / (low + 1) : large + (tile - in_large) / low);
+        };
+        const int first = cta_of(rec->tile);
+        rec->count = cta_of(rec->tile + rec->count - 1) - first + 1;
+        rec->first = first;
+      }
     } else if (warp == 1) {
       // ---------------- products ----------------
       const uint32_t go = elect_one();
@@ -1289,45 +1300,79 @@ __global__ void __launch_bounds__(256) prefix_finish_kernel(const PrefixParams p
     return;
   }
   if (w0 == 0 && lane == 0 && p.status && p.head->status) atomicOr(p.status, p.head->status);
-  // the pieces of the unit that CTA blockIdx.x has the first one of
-  const SplitRec rec = p.recs[blockIdx.x];
-  if (rec.pieces > 0) {
-    constexpr int N = D / 32;
-    struct alignas(4 * N) Values {
-      float v[N];
-    };
-    struct alignas(2 * N) Outputs {
-      T v[N];
-    };
-    const long long first = (long long)blockIdx.x * 2 + 1;
-    auto slot = [&](int i, int r) { return (i == 0 ? first : 2LL * (blockIdx.x + i)) * kUnitRows + r; };
-    for (int r = blockIdx.y * 8 + wp; r < rec.rows; r += gridDim.y * 8) {
-      float m = -INFINITY;
-      for (int i = 0; i <= rec.pieces; ++i) m = fmaxf(m, p.part_ml[slot(i, r)].x);
-      const float ref = m == -INFINITY ? 0.f : m;
-      float l = 0.f, o[N] = {};
-      for (int i = 0; i <= rec.pieces; ++i) {
-        const float2 ml = p.part_ml[slot(i, r)];
-        const Values x = reinterpret_cast<const Values*>(p.part_o + slot(i, r) * D)[lane];
-        const float f = ex2_approx(ml.x - ref);
-        l = fmaf(ml.y, f, l);
-#pragma unroll
-        for (int z = 0; z < N; ++z) o[z] = fmaf(x.v[z], f, o[z]);
-      }
+  // The CTAs that have the pieces of a unit join its rows, each its share: one long prefix is split over all of them
+  // (two units of 98 pieces, joined by their first CTAs alone: 49 us the call, 32 this way).
+  constexpr int N = D / 32;
+  struct alignas(4 * N) Values {
+    float v[N];
+  };
+  struct alignas(2 * N) Outputs {
+    T v[N];
+  };
+  const SplitRec begins_in = p.recs[2 * blockIdx.x], ends_in = p.recs[2 * blockIdx.x + 1];
+#pragma unroll 1
+  for (int which = 0; which < 2; ++which) {
+    const SplitRec rec = which ? ends_in : begins_in;
+    if (rec.count == 0) continue;
+    auto slot = [&](int i, int r) { return ((long long)(rec.first + i) * 2 + (i == 0)) * kUnitRows + r; };
+    // (at most 128 rows, 2^16 CTAs; two pieces are the first one's)
+    const uint32_t share = blockIdx.x - rec.first, shares = rec.count > 2 ? rec.count : 1;
+    if (share >= shares) continue;
+    const int r_begin = (int)(rec.rows * share / shares), r_end = (int)(rec.rows * (share + 1) / shares);
+    auto values = [&](int i, int r) { return reinterpret_cast<const Values*>(p.part_o + slot(i, r) * D)[lane]; };
+    auto put = [&](int r, float m, float l, float* o) {
       const int rr = rec.r0 + r;
       const long long w = (long long)(rec.t0 + rr / p.hr) * p.hq + rec.head * p.hr + rr % p.hr;
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-      for (int z = 0; z < N; ++z) o[z] *= inv;
       if (!(l == l)) {
         row_by_keys<T, D>(p, w, sq[wp]);
-        continue;
+        return;
       }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
       Outputs y;
 #pragma unroll
-      for (int z = 0; z < N; ++z) y.v[z] = Elem<T>::put(o[z]);
+      for (int z = 0; z < N; ++z) y.v[z] = Elem<T>::put(o[z] * inv);
       reinterpret_cast<Outputs*>(reinterpret_cast<T*>(p.out) + w * D)[lane] = y;
       if (p.lse && lane == 0) p.lse[w] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
+    };
+#pragma unroll 1
+    for (int r = r_begin + blockIdx.y * 8 + wp; r < r_end; r += gridDim.y * 8) {
+      float o[N];
+      if (rec.count == 2) {
+        const Values x0 = values(0, r), x1 = values(1, r);
+        const float2 a = p.part_ml[slot(0, r)], b = p.part_ml[slot(1, r)];
+        const float m = fmaxf(a.x, b.x), ref = m == -INFINITY ? 0.f : m, f0 = ex2_approx(a.x - ref), f1 = ex2_approx(b.x - ref);
+#pragma unroll
+        for (int z = 0; z < N; ++z) o[z] = fmaf(x1.v[z], f1, x0.v[z] * f0);
+        put(r, m, fmaf(b.y, f1, a.y * f0), o);
+        continue;
+      }
+      // statistics of 32 pieces, a lane each
+      auto stats = [&](int i) { return i < rec.count ? p.part_ml[slot(i, r)] : make_float2(-INFINITY, 0.f); };
+      float m = -INFINITY, l = 0.f, f = 0.f;
+#pragma unroll 1
+      for (int i = lane; i < rec.count; i += 32) m = fmaxf(m, stats(i).x);
+#pragma unroll
+      for (int z = 16; z > 0; z >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, z));
+      const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int z = 0; z < N; ++z) o[z] = 0.f;
+#pragma unroll 1
+      for (int i0 = 0; i0 < rec.count; i0 += 32) {
+        const float2 ml = stats(i0 + lane);
+        f = ex2_approx(ml.x - ref);
+        l = fmaf(ml.y, f, l);
+        const int n = min(32, rec.count - i0);
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+          const Values x = values(i0 + i, r);
+          const float fi = __shfl_sync(0xffffffffu, f, i);
+#pragma unroll
+          for (int z = 0; z < N; ++z) o[z] = fmaf(x.v[z], fi, o[z]);
+        }
+      }
+#pragma unroll
+      for (int z = 16; z > 0; z >>= 1) l += __shfl_xor_sync(0xffffffffu, l, z);
+      put(r, m, l, o);
     }
   }
   const int listed = p.head->listed;
@@ -1383,7 +1428,7 @@ Layout layout(const fe_prefix_args* a, int ctas, int max_tiles) {
   w.gcost = take(8 * ((size_t)a->n_groups + 1));
   w.cost = take(4 * (size_t)max_tiles);
   w.before = take(8 * ((size_t)max_tiles + 1));
-  w.recs = take(sizeof(SplitRec) * ctas);
+  w.recs = take(sizeof(SplitRec) * 2 * ctas);
   w.list = take(4 * (size_t)kListed);
   w.part_o = take((size_t)ctas * 2 * kUnitRows * a->kv.head_dim * 4);
   w.part_ml = take((size_t)ctas * 2 * kUnitRows * 8);
@@ -1442,7 +1487,7 @@ cudaError_t prefix_go(const PageMaps& m, const PrefixParams& p, cudaStream_t s) 
   cudaError_t e = launch_k(prefix_plan_kernel, dim3(kPlanCtas), dim3(kPlanThreads), 0, s, p);
   if (e == cudaSuccess)
     e = launch_k(prefix_attend_kernel<T, D>, dim3((unsigned)p.ctas), dim3(C::kThreads), C::kSmem, s, m, p);
-  if (e == cudaSuccess) e = launch_k(prefix_finish_kernel<T, D>, dim3((unsigned)p.ctas, 4), dim3(256), 0, s, p);
+  if (e == cudaSuccess) e = launch_k(prefix_finish_kernel<T, D>, dim3((unsigned)p.ctas, 2), dim3(256), 0, s, p);
   return e;
 }
 template <typename T>
