@@ -282,6 +282,9 @@ struct PrefixCfg {
   static constexpr uint32_t kCols = 256, kP = kOwnP ? 128 : 0, kO = kOwnP ? 192 : 128;
   static_assert(kO + D <= kCols, "TMEM budget");
   static constexpr int ND = 6;  // tile descriptors in flight
+  // Weights of a tile that all rows see, so many keys at a time: short code goes faster as long as the next product
+  // does not wait for P's columns (D = 128: 424 us a long reading by 32, 447 by 16; others 1 % the other way).
+  static constexpr int kStep = kOwnP ? 16 : 32;
   static constexpr int kBars = 3 * NV + 2 * NK + 2 * ND + 2 * NQ + 3 + kUnitsAhead + 1;
   static constexpr size_t kFixed = sizeof(TileDesc) * ND + sizeof(UnitInfo) * kUnitsAhead + sizeof(RowInfo) * 128 * NQ +
                                    sizeof(Dirty) * kUnitsAhead + 8 * kBars + 16;
@@ -995,10 +998,10 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
           };
           if (whole) {
 #pragma unroll 1
-            for (int c0 = 0; c0 < 128; c0 += 64) {
-              float v[64];
-              tmem_ld64(t_s + (uint32_t)c0, v);
-              mx = fmaxf(mx, maxn<64>(v));
+            for (int c0 = 0; c0 < 128; c0 += 32) {
+              float v[32];
+              tmem_ld32(t_s + (uint32_t)c0, v);
+              mx = fmaxf(mx, maxn<32>(v));
             }
           } else {
             // this row's keys of a slot: of the prefix all valid ones, of its own sequence those up to itself
@@ -1024,23 +1027,18 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
             if (single) {
               // every row of the warp sees one slot at most (short sequences): 16 scores each, picked from the pairs
               slot = __ffs(mask) - 1;
-              const int n = slot < 0 ? 0 : (int)(((slot < 4 ? seen0 : seen1) >> (8 * (slot & 3))) & 0xffu);
+              const uint32_t bits = slot < 0 ? 0u : (1u << (((slot < 4 ? seen0 : seen1) >> (8 * (slot & 3))) & 0xffu)) - 1u;
 #pragma unroll
               for (int i = 0; i < kSlot; ++i) one[i] = -INFINITY;
 #pragma unroll 1
-              for (uint32_t left = pairs; left; left &= left - 1) {
+              for (uint32_t left = any; left; left &= left - 1) {
                 const int z = __ffs(left) - 1;
-                float v[32];
-                tmem_ld32(t_s + (uint32_t)(32 * z), v);
+                float v[kSlot];
+                tmem_ld16(t_s + (uint32_t)(kSlot * z), v);
+                const uint32_t here = slot == z ? bits : 0u;
 #pragma unroll
-                for (int i = 0; i < kSlot; ++i) {
-                  if (slot == 2 * z) one[i] = v[i];
-                  if (slot == 2 * z + 1) one[i] = v[kSlot + i];
-                }
-              }
-#pragma unroll
-              for (int i = 0; i < kSlot; ++i) {
-                if (i >= n) one[i] = -INFINITY;
+                for (int i = 0; i < kSlot; ++i)
+                  if (here & (1u << i)) one[i] = v[i];
               }
               mx = maxn<kSlot>(one);
             } else {
@@ -1099,28 +1097,28 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
           const std::integral_constant<int, 32> c32{};
           if (whole) {
 #pragma unroll 1
-            for (int c0 = 0; c0 < 128; c0 += 64) {
-              float v[64];
-              tmem_ld64(t_s + (uint32_t)c0, v);
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                uint32_t pk[16];
-                weights(v + 32 * h, c32, pk);
-                tmem_st16_nowait(t_p + (uint32_t)(c0 / 2 + 16 * h), pk);
+            for (int c0 = 0; c0 < 128; c0 += C::kStep) {
+              float v[C::kStep];
+              uint32_t pk[C::kStep / 2];
+              if constexpr (C::kStep == 32) {
+                tmem_ld32(t_s + (uint32_t)c0, v);
+                weights(v, std::integral_constant<int, 32>(), pk);
+                tmem_st16_nowait(t_p + (uint32_t)(c0 / 2), pk);
+              } else {
+                tmem_ld16(t_s + (uint32_t)c0, v);
+                weights(v, std::integral_constant<int, 16>(), pk);
+                tmem_st8_nowait(t_p + (uint32_t)(c0 / 2), pk);
               }
             }
           } else if (single) {
             uint32_t mine8[kSlot / 2];
             weights(one, std::integral_constant<int, kSlot>(), mine8);
 #pragma unroll 1
-            for (int z = 0; 2 * z < slots; ++z) {
-              uint32_t pk[16];
+            for (int z = 0; z < slots; ++z) {
+              uint32_t pk[kSlot / 2];
 #pragma unroll
-              for (int i = 0; i < kSlot / 2; ++i) {
-                pk[i] = slot == 2 * z ? mine8[i] : 0u;
-                pk[kSlot / 2 + i] = slot == 2 * z + 1 ? mine8[i] : 0u;
-              }
-              tmem_st16_nowait(t_p + (uint32_t)(16 * z), pk);
+              for (int i = 0; i < kSlot / 2; ++i) pk[i] = slot == z ? mine8[i] : 0u;
+              tmem_st8_nowait(t_p + (uint32_t)(kSlot / 2 * z), pk);
             }
           } else {
 #pragma unroll 1
@@ -1177,22 +1175,22 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
         tc_fence_after();
       }
 #pragma unroll 1
-      for (int c0 = 0; c0 < D; c0 += 32) {
-        float o[32];
+      for (int c0 = 0; c0 < D; c0 += 16) {
+        float o[16];
         if (mine > 0) {
-          tmem_ld32(t_o + (uint32_t)c0, o);
+          tmem_ld16(t_o + (uint32_t)c0, o);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] *= f;
+          for (int i = 0; i < 16; ++i) o[i] *= f;
         } else {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = 0.f;
+          for (int i = 0; i < 16; ++i) o[i] = 0.f;
         }
         if (store && direct) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 8) *reinterpret_cast<uint4*>(out + c0 + i) = piece_put<T>(o + i);
+          for (int i = 0; i < 16; i += 8) *reinterpret_cast<uint4*>(out + c0 + i) = piece_put<T>(o + i);
         } else if (store) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 8) st_sector(part + c0 + i, o + i);
+          for (int i = 0; i < 16; i += 8) st_sector(part + c0 + i, o + i);
         }
       }
       tc_fence_before();
