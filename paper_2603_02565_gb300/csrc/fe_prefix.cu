@@ -661,7 +661,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
           tc_fence_after();
           const uint64_t vd = vd0 + (uint64_t)((pr.i * C::kTile) >> 4);
           umma_bf16_tmem_a_if(t_o, t_p, vd, idesc_pv, p_first ? 0u : 1u, go);
-          if (p_slots == kSlots) {
+          if (D == 128 && p_slots == kSlots) {
 #pragma unroll
             for (int s = 1; s < kSlots; ++s)
               umma_bf16_tmem_a_if(t_o, t_p + (uint32_t)(8 * s), vd + (uint64_t)((s * kSlot * C::kRow) >> 4), idesc_pv, 1u, go);
@@ -904,7 +904,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
           const int pc = lane % NP;
           const uint32_t to = smem_u32(sQ) + qr.i * C::kTile + (uint32_t)(pc * 16) / C::kRow * C::kHalf;
           const uint32_t poff = (uint32_t)(pc * 16) % C::kRow;
-#pragma unroll 4
+#pragma unroll (D == 128 ? 4 : 1)
           for (int r = lane / NP; r < u.rows; r += RP) {
             int t, h;
             at(r, t, h);
@@ -1008,7 +1008,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
             const int4 *own4 = reinterpret_cast<const int4*>(td->owner), *base4 = reinterpret_cast<const int4*>(td->base),
                        *count4 = reinterpret_cast<const int4*>(td->count);
             uint32_t mask = 0;
-#pragma unroll
+#pragma unroll 1
             for (int h = 0; h < 2; ++h) {
               const int4 ow = own4[h], ba = base4[h], co = count4[h];
               auto n_of = [&](int owner, int base, int count) {
