@@ -46,7 +46,6 @@ struct PlanHead {
   int status;   // ST_ bits of this call
   int bad;      // the row or group offsets are not what they must be: all rows NaN
   int listed;   // rows to compute again (more than kListed: all rows are looked at)
-  int n_tiles;  // row tiles (units per key head)
 };
 // A split unit: its rows, and the CTAs that have its pieces (count 0: none).  While the schedule runs, count is its
 // tiles, the first of them tile.
@@ -64,7 +63,7 @@ struct PrefixParams {
   int64_t q_row, q_head;
   int n_groups, n_seqs, n_rows, hq, hkv, hr, hr_inv, prefix_cols, page_cols, page_rows, page_shift, n_pages;
   float scale, sc;  // sc: scale log2(e), and no 0 (masked scores, -inf, are multiplied by it)
-  int ctas, max_tiles;
+  int ctas;
   // workspace
   PlanHead* head;
   int2* tok;           // [n_rows] sequence of a row, and how many of its own rows it sees (-1: a length is none)
@@ -153,7 +152,7 @@ __global__ void __launch_bounds__(kPlanThreads) __cluster_dims__(kPlanCtas, 1, 1
 #pragma unroll 4
   for (int s = tid; s < p.n_seqs; s += kPlanThreads) bad |= p.row_start[s] > p.row_start[s + 1];
   bad = __syncthreads_or(bad);  // (the same in every CTA)
-  if (all == 0) *p.head = PlanHead{0, bad ? 1 : 0, 0, 0};
+  if (all == 0) *p.head = PlanHead{0, bad ? 1 : 0, 0};
   if (bad) return;
   // (the groups' first sequences are searched for every sequence: in shared memory, if they fit)
   const int32_t* groups = p.group_start;
@@ -177,10 +176,7 @@ __global__ void __launch_bounds__(kPlanThreads) __cluster_dims__(kPlanCtas, 1, 1
     tiles += sh_i[31];
     __syncthreads();
   }
-  if (all == 0) {
-    p.gtile[p.n_groups] = tiles;
-    p.head->n_tiles = tiles;
-  }
+  if (all == 0) p.gtile[p.n_groups] = tiles;
   for (int i = all; i < tiles; i += kAll) p.cost[i] = 0;
   // what the rows see
   for (int t = all; t < p.n_rows; t += kAll) {
@@ -305,6 +301,9 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t saddr, uint32_t lbo, uint
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -534,12 +533,14 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
             if (next < plen) ahead_page = __ldg(pre_table + (next >> p.page_shift));
           } else {
             const int slot = (tile - ptiles) * kSlots + lane;
+            int from = -1;  // the chunk to be opened
             if (!own_open) {
               own_open = true;
-              const int f = s0 + warp_find_row(p.row_start + s0, s1 - s0, ta);
-              chunk(f, 0);
+              from = s0 + warp_find_row(p.row_start + s0, s1 - s0, ta);
+              c_end = 0;
             }
             while (true) {
+              if (from >= 0) chunk(from, c_end);
               // the chunk's sequence with the last first slot at or before this lane's (empty ones lie before it)
               int at = 0;
 #pragma unroll
@@ -556,7 +557,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
               }
               // past the chunk's end: the next one, as long as its sequences have rows here
               if (!__any_sync(0xffffffffu, b_owner == -2 && slot >= c_end) || cs + 32 >= s1 || p.row_start[cs + 32] > tb) break;
-              chunk(cs + 32, c_end);
+              from = cs + 32;
             }
           }
           if (b_owner != -2) {
@@ -891,13 +892,6 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
             t = u.t0 + t_first + (p.hr == 1 ? r : q);
             h = u.head * p.hr + (p.hr == 1 ? 0 : h_first + r - q * p.hr);
           };
-          int2 k[4];  // what the rows see
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            int t, h;
-            at(lane + 32 * i, t, h);
-            k[i] = lane + 32 * i < u.rows ? __ldg(p.tok + t) : make_int2(-5, 0);
-          }
           if (!wait(q_free + qr.i, qr.par ^ 1u)) break;
           // the queries: pieces of 16 bytes, swizzled as TMA would have it
           constexpr int NP = D / 8, RP = 32 / NP;  // pieces of a row, rows of a step
@@ -913,11 +907,16 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
                        reinterpret_cast<const T*>(p.q) + (long long)t * p.q_row + h * p.q_head + pc * 8);
           }
           RowInfo* info = rinfo + qr.i * 128;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            int t, h;
-            at(lane + 32 * i, t, h);
-            info[lane + 32 * i] = RowInfo{k[i].x, k[i].y, k[i].x < 0 ? -1 : t * p.hq + h, 0};
+#pragma unroll 1
+          for (int r = lane; r < kUnitRows; r += 32) {
+            if (r < u.rows) {
+              int t, h;
+              at(r, t, h);
+              cp_async8(smem_u32(info + r), p.tok + t);
+              info[r].out = t * p.hq + h;
+            } else {
+              info[r] = RowInfo{-5, 0, -1, 0};
+            }
           }
           // (announced as a tile's slots are)
           cp_async_commit();
@@ -990,7 +989,6 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
           auto pair = [&](int z, float* v) {  // scores of slots 2 z and 2 z + 1, unseen ones -inf
             tmem_ld32(t_s + (uint32_t)(32 * z), v);
             const uint32_t two = (z < 2 ? seen0 : seen1) >> (16 * (z & 1));
-            if (__all_sync(0xffffffffu, (two & 0xffffu) == 0x1010u)) return;
             const uint32_t bits = ((1u << (two & 0xff)) - 1u) | ((1u << ((two >> 8) & 0xff)) - 1u) << kSlot;
 #pragma unroll
             for (int i = 0; i < 2 * kSlot; ++i)
@@ -1517,8 +1515,7 @@ extern "C" int fe_prefix_attention(const fe_prefix_args* a, void* stream) {
   if (dev.err != cudaSuccess) return fail_cuda(dev.err, "fe_prefix_attention");
   PrefixParams p{};
   p.ctas = 2 * dev.sms;
-  p.max_tiles = most_tiles(a);
-  const Layout w = layout(a, p.ctas, p.max_tiles);
+  const Layout w = layout(a, p.ctas, most_tiles(a));
   if (a->workspace_bytes < w.bytes) return fail(FE_ERR_WORKSPACE, "workspace too small");
   char* ws = static_cast<char*>(a->workspace);
   p.head = reinterpret_cast<PlanHead*>(ws + w.head);
