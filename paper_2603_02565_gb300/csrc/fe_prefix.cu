@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kPlanThreads) __cluster_dims__(kPlanCtas, 1, 1
   bool bad = p.row_start[0] != 0 || p.row_start[p.n_seqs] != p.n_rows || p.group_start[0] != 0 ||
              p.group_start[p.n_groups] != p.n_seqs;
   for (int g = tid; g < p.n_groups; g += kPlanThreads) bad |= p.group_start[g] > p.group_start[g + 1];
-#pragma unroll 4
+#pragma unroll 8
   for (int s = tid; s < p.n_seqs; s += kPlanThreads) bad |= p.row_start[s] > p.row_start[s + 1];
   bad = __syncthreads_or(bad);  // (the same in every CTA)
   if (all == 0) *p.head = PlanHead{0, bad ? 1 : 0, 0};
@@ -178,9 +178,16 @@ __global__ void __launch_bounds__(kPlanThreads) __cluster_dims__(kPlanCtas, 1, 1
   }
   if (all == 0) p.gtile[p.n_groups] = tiles;
   for (int i = all; i < tiles; i += kAll) p.cost[i] = 0;
+  // The sequence of a row: where it would be if all had as many rows, or the next one, or else searched for.
+  const float per_row = (float)p.n_seqs / (float)p.n_rows;
+  auto seq_of = [&](int t) {
+    const int s = min(p.n_seqs - 1, (int)((float)t * per_row));
+    const int a = p.row_start[s], b = p.row_start[s + 1], c = p.row_start[min(s + 2, p.n_seqs)];
+    return a <= t && t < b ? s : b <= t && t < c ? s + 1 : find_last(p.row_start, p.n_seqs, t);
+  };
   // what the rows see
   for (int t = all; t < p.n_rows; t += kAll) {
-    const int s = find_last(p.row_start, p.n_seqs, t), a = p.row_start[s], len = p.seq_len[s];
+    const int s = seq_of(t), a = p.row_start[s], len = p.seq_len[s];
     const int g = find_last(groups, p.n_groups, s);
     const bool fine = len_ok(p, len) && prefix_ok(p, p.prefix_len[g]);
     p.tok[t] = make_int2(s, fine ? seen_rows(len, p.row_start[s + 1] - a, t - a) : -1);
@@ -204,7 +211,7 @@ __global__ void __launch_bounds__(kPlanThreads) __cluster_dims__(kPlanCtas, 1, 1
     const int g = find_last(p.gtile, p.n_groups, rt), i = rt - p.gtile[g];
     if (i == 0) continue;
     const int first = p.row_start[groups[g]], t = first + (int)((long long)i * kUnitRows / p.hr);
-    const int s = find_last(p.row_start, p.n_seqs, t), a = p.row_start[s];
+    const int s = seq_of(t), a = p.row_start[s];
     if ((long long)(a - first) * p.hr / kUnitRows < i) {
       const int c = slots(s, a, p.row_start[s + 1] - a, first, i);
       if (c) atomicAdd(p.cost + rt, c);
@@ -709,7 +716,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
           const int qi = qr.i == 0 ? NQ - 1 : qr.i - 1;
           const uint64_t qd = qd0 + (uint64_t)((qi * C::kTile) >> 4), kd = kd0 + (uint64_t)((kr.i * C::kTile) >> 4);
           const uint32_t id = idesc | ((uint32_t)(slots * 2) << 17);
-#pragma unroll
+#pragma unroll (D == 128 ? 8 : 1)
           for (int kk = 0; kk < D / 16; ++kk) {
             const uint64_t at = (uint64_t)(((kk * 32) / C::kRow * C::kHalf + (kk * 32) % C::kRow) >> 4);
             umma_bf16_if(tmem, qd + at, kd + at, id, kk != 0 ? 1u : 0u, go);
