@@ -19,13 +19,27 @@
 // A CTA of the attend kernel has four softmax warps (a row a thread) and four that feed
 // them: one walks the schedule, one issues tcgen05.mma (S = Q K^T, and O += P V with P from
 // TMEM), one loads queries and keys, one loads values and looks through them.  S, P and O
-// live in half of the SM's TMEM.  What such a warp does is a chain of short steps, some
-// five cycles an instruction: the two CTAs fill each other's gaps.  (One CTA per SM with two
-// groups of softmax warps, on alternate tiles or on 256 rows, joined at the unit's end,
-// had the same steps in one chain for both.)
+// live in half of the SM's TMEM.  What such a warp does is a chain of short steps: the two
+// CTAs fill each other's gaps.  (One CTA per SM with two groups of softmax warps, on
+// alternate tiles or on 256 rows, joined at the unit's end, had the same steps in one chain
+// for both.)  Eight unlike roles compete for the instruction cache: a third of all stalls
+// were for instructions while loops were unrolled; rolled ones took a quarter off.
+//
+// Device time of a call:
+//   4 groups x 16 sequences, a token each, prefixes up to 32768 keys, 32 heads of 8 x 128:
+//     113 us, 4.2 TB/s.  Bound by how much a CTA has in flight: reads alone, 64 KB in flight
+//     an SM, reach 5.1 TB/s in boxes of 64 rows (a copy 6.8);
+//   2 groups x 8 sequences, up to 256 rows each, prefixes of 8192, the same heads:
+//     412 us, 1130 TFLOP/s (cuBLAS 1895).  The products take half of the time, the chain
+//     scores - maximum - weights - product of two CTAs the rest;
+//   256 groups x 50 sequences, a token each, prefixes of 256, 4 heads of 32: 89 us (bytes
+//     alone 9): a tile's steps again, each of few instructions per byte;
+//   1 group x 4 sequences, prefix of 300, 8 heads of 64: 17 us, of which three launches 8.
+// A tile of 128 keys costs each row 128 exponentials, at sixteen a clock and SM 1.1 us for the
+// tiles of both CTAs: no head dimension of 32 or 64 can go below that.
 //
 // 0 x NaN is NaN, so a value that is no number spoils rows that give it no weight.  The
-// cleaning warp clears the value rows past a sequence's end, whatever the pages hold there,
+// values' warp clears the value rows past a sequence's end, whatever the pages hold there,
 // and looks through tiles of own keys, which rows of other sequences (and earlier rows of
 // the same one) do not see: infinities and NaN there become 0 in the tile, and all rows of
 // the sequence that has them are computed again from their visible keys alone.  Nothing is
@@ -245,7 +259,7 @@ __global__ void __launch_bounds__(kPlanThreads) __cluster_dims__(kPlanCtas, 1, 1
 // ---------------------------------------------------------------------------
 // attend
 // ---------------------------------------------------------------------------
-// What the loading warp tells the others about a key tile
+// What the schedule tells the others about a key tile
 struct alignas(16) TileDesc {
   int flags, slots, bad, piece, pad[4];
   int owner[kSlots];  // sequence, or -1: the prefix
