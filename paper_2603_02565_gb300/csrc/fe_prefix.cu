@@ -103,7 +103,7 @@ __device__ __forceinline__ int seen_rows(int len, int n, int j) { return max(0, 
 // ---------------------------------------------------------------------------
 // plan
 // ---------------------------------------------------------------------------
-constexpr int kPlanThreads = 1024, kPlanGroups = 4096, kPlanCtas = 8;
+constexpr int kPlanThreads = 1024, kPlanGroups = 2048, kPlanCtas = 8;
 static_assert(kPlanThreads == 1024, "block_scan sums the totals of 32 warps");
 
 // inclusive sum over the block's threads
@@ -154,7 +154,7 @@ __device__ __forceinline__ void plan_barrier() {  // of the cluster, global writ
 __global__ void __launch_bounds__(kPlanThreads) __cluster_dims__(kPlanCtas, 1, 1) prefix_plan_kernel(const PrefixParams p) {
   __shared__ long long sh[32];
   __shared__ int sh_i[32];
-  __shared__ int sh_groups[kPlanGroups];
+  __shared__ int sh_groups[kPlanGroups], sh_first[kPlanGroups], sh_tile[kPlanGroups];
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x, all = blockIdx.x * kPlanThreads + tid;
@@ -168,24 +168,31 @@ __global__ void __launch_bounds__(kPlanThreads) __cluster_dims__(kPlanCtas, 1, 1
   bad = __syncthreads_or(bad);  // (the same in every CTA)
   if (all == 0) *p.head = PlanHead{0, bad ? 1 : 0, 0};
   if (bad) return;
-  // (the groups' first sequences are searched for every sequence: in shared memory, if they fit)
-  const int32_t* groups = p.group_start;
-  if (p.n_groups <= kPlanGroups) {
-    for (int g = tid; g < p.n_groups; g += kPlanThreads) sh_groups[g] = p.group_start[g];
-    groups = sh_groups;
-    __syncthreads();
-  }
+  // The groups' first sequences, rows and row tiles: in shared memory, if they fit, because every sequence looks for
+  // its group.
+  const bool few = p.n_groups <= kPlanGroups;
+  const int32_t* groups = few ? sh_groups : p.group_start;
+  const int* gtile = few ? sh_tile : p.gtile;
+  auto first_row = [&](int g) { return few ? sh_first[g] : p.row_start[p.group_start[g]]; };
   // row tiles of the groups (every CTA sums them up for itself, the first one writes them)
   int tiles = 0;
   for (int g0 = 0; g0 < p.n_groups; g0 += kPlanThreads) {
     const int g = g0 + tid;
     int n = 0;
     if (g < p.n_groups) {
-      const long long rows = (long long)(p.row_start[p.group_start[g + 1]] - p.row_start[groups[g]]) * p.hr;
+      const int s = p.group_start[g], a = p.row_start[s];
+      const long long rows = (long long)(p.row_start[p.group_start[g + 1]] - a) * p.hr;
       n = (int)((rows + kUnitRows - 1) / kUnitRows);
+      if (few) {
+        sh_groups[g] = s;
+        sh_first[g] = a;
+      }
     }
     const int incl = block_scan(n, sh_i);
-    if (g < p.n_groups && blockIdx.x == 0) p.gtile[g] = tiles + incl - n;
+    if (g < p.n_groups) {
+      if (few) sh_tile[g] = tiles + incl - n;
+      if (blockIdx.x == 0) p.gtile[g] = tiles + incl - n;
+    }
     __syncthreads();
     tiles += sh_i[31];
     __syncthreads();
@@ -199,32 +206,25 @@ __global__ void __launch_bounds__(kPlanThreads) __cluster_dims__(kPlanCtas, 1, 1
     const int a = p.row_start[s], b = p.row_start[s + 1], c = p.row_start[min(s + 2, p.n_seqs)];
     return a <= t && t < b ? s : b <= t && t < c ? s + 1 : find_last(p.row_start, p.n_seqs, t);
   };
-  // what the rows see
-  for (int t = all; t < p.n_rows; t += kAll) {
-    const int s = seq_of(t), a = p.row_start[s], len = p.seq_len[s];
-    const int g = find_last(groups, p.n_groups, s);
-    const bool fine = len_ok(p, len) && prefix_ok(p, p.prefix_len[g]);
-    p.tok[t] = make_int2(s, fine ? seen_rows(len, p.row_start[s + 1] - a, t - a) : -1);
-  }
   plan_barrier();
   // slots of own keys: a sequence's first row tile by the sequence, its further ones by the tile
   auto slots = [&](int s, int a, int n, int first, int i) {  // sequence s (its n rows from a on, the group's from first on) in tile i
     const int len = p.seq_len[s];
-    const int j = min(n - 1, (int)(((long long)(i + 1) * kUnitRows - 1) / p.hr) - (a - first));
+    const int j = min(n - 1, (int)(((uint32_t)(i + 1) * kUnitRows - 1) / (uint32_t)p.hr) - (a - first));  // (rows * hr < 2^31)
     return len_ok(p, len) ? (seen_rows(len, n, j) + kSlot - 1) / kSlot : 0;
   };
   for (int s = all; s < p.n_seqs; s += kAll) {
     const int a = p.row_start[s], n = p.row_start[s + 1] - a;
     if (n == 0) continue;
-    const int g = find_last(groups, p.n_groups, s), first = p.row_start[groups[g]];
+    const int g = find_last(groups, p.n_groups, s), first = first_row(g);
     const int i = (int)((long long)(a - first) * p.hr / kUnitRows);
     const int c = slots(s, a, n, first, i);
-    if (c) atomicAdd(p.cost + p.gtile[g] + i, c);
+    if (c) atomicAdd(p.cost + gtile[g] + i, c);
   }
   for (int rt = all; rt < tiles; rt += kAll) {
-    const int g = find_last(p.gtile, p.n_groups, rt), i = rt - p.gtile[g];
+    const int g = find_last(gtile, p.n_groups, rt), i = rt - gtile[g];
     if (i == 0) continue;
-    const int first = p.row_start[groups[g]], t = first + (int)((long long)i * kUnitRows / p.hr);
+    const int first = first_row(g), t = first + (int)((uint32_t)i * kUnitRows / (uint32_t)p.hr);
     const int s = seq_of(t), a = p.row_start[s];
     if ((long long)(a - first) * p.hr / kUnitRows < i) {
       const int c = slots(s, a, p.row_start[s + 1] - a, first, i);
@@ -232,14 +232,23 @@ __global__ void __launch_bounds__(kPlanThreads) __cluster_dims__(kPlanCtas, 1, 1
     }
   }
   plan_barrier();
-  if (blockIdx.x != 0) return;
+  if (blockIdx.x != 0) {
+    // what the rows see, while the first CTA sums up
+    for (int t = all - kPlanThreads; t < p.n_rows; t += kAll - kPlanThreads) {
+      const int s = seq_of(t), a = p.row_start[s], len = p.seq_len[s];
+      const int g = find_last(groups, p.n_groups, s);
+      const bool fine = len_ok(p, len) && prefix_ok(p, p.prefix_len[g]);
+      p.tok[t] = make_int2(s, fine ? seen_rows(len, p.row_start[s + 1] - a, t - a) : -1);
+    }
+    return;
+  }
   // key tiles of the row tiles, and those before them
   long long run = 0;
   for (int r0 = 0; r0 < tiles; r0 += kPlanThreads) {
     const int rt = r0 + tid;
     long long c = 0;
     if (rt < tiles) {
-      const int g = find_last(p.gtile, p.n_groups, rt), n = p.prefix_len[g];
+      const int g = find_last(gtile, p.n_groups, rt), n = p.prefix_len[g];
       const int own = *reinterpret_cast<volatile int*>(p.cost + rt);  // (summed in L2)
       c = ((prefix_ok(p, n) ? n : 0) + kTileKeys - 1) / kTileKeys + (own + kSlots - 1) / kSlots;
       c = c < 1 ? 1 : c;
