@@ -27,12 +27,12 @@
 //
 // Device time of a call:
 //   4 groups x 16 sequences, a token each, prefixes up to 32768 keys, 32 heads of 8 x 128:
-//     113 us, 4.2 TB/s.  Bound by how much a CTA has in flight: reads alone, 64 KB in flight
+//     112 us, 4.3 TB/s.  Bound by how much a CTA has in flight: reads alone, 64 KB in flight
 //     an SM, reach 5.1 TB/s in boxes of 64 rows (a copy 6.8);
 //   2 groups x 8 sequences, up to 256 rows each, prefixes of 8192, the same heads:
-//     412 us, 1130 TFLOP/s (cuBLAS 1895).  The products take half of the time, the chain
+//     411 us, 1130 TFLOP/s (cuBLAS 1895).  The products take half of the time, the chain
 //     scores - maximum - weights - product of two CTAs the rest;
-//   256 groups x 50 sequences, a token each, prefixes of 256, 4 heads of 32: 89 us (bytes
+//   256 groups x 50 sequences, a token each, prefixes of 256, 4 heads of 32: 87 us (bytes
 //     alone 9): a tile's steps again, each of few instructions per byte;
 //   1 group x 4 sequences, prefix of 300, 8 heads of 64: 17 us, of which three launches 8.
 // A tile of 128 keys costs each row 128 exponentials, at sixteen a clock and SM 1.1 us for the
