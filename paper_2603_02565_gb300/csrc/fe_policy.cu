@@ -530,15 +530,15 @@ cudaError_t policy_go(const PolicyParams& p, cudaStream_t s) {
   const int pieces = (p.vocab + N - 1) / N;
   // a gradient whose rows start elsewhere between two 16-byte boundaries cannot leave in 16-byte pieces
   const bool aligned = !p.grad || ((((uintptr_t)p.grad ^ (uintptr_t)p.logits) & 15) == 0 && (p.grad_row - p.logits_row) % N == 0);
-  if (aligned && pieces <= 4096) {
+  if (aligned && pieces <= 512 * 8) {  // a CTA's threads by the pieces that each holds
     const dim3 g((unsigned)p.rows);
-    if (pieces <= 128) return launch_k(policy_row_kernel<T, 32, 4>, g, dim3(32), 0, s, p);
-    if (pieces <= 256) return launch_k(policy_row_kernel<T, 64, 4>, g, dim3(64), 0, s, p);
-    if (pieces <= 512) return launch_k(policy_row_kernel<T, 128, 4>, g, dim3(128), 0, s, p);
-    if (pieces <= 1024) return launch_k(policy_row_kernel<T, 128, 8>, g, dim3(128), 0, s, p);
-    if (pieces <= 1536) return launch_k(policy_row_kernel<T, 256, 6>, g, dim3(256), 0, s, p);
-    if (pieces <= 2048) return launch_k(policy_row_kernel<T, 256, 8>, g, dim3(256), 0, s, p);
-    if (pieces <= 3072) return launch_k(policy_row_kernel<T, 512, 6>, g, dim3(512), 0, s, p);
+    if (pieces <= 32 * 4) return launch_k(policy_row_kernel<T, 32, 4>, g, dim3(32), 0, s, p);
+    if (pieces <= 64 * 4) return launch_k(policy_row_kernel<T, 64, 4>, g, dim3(64), 0, s, p);
+    if (pieces <= 128 * 4) return launch_k(policy_row_kernel<T, 128, 4>, g, dim3(128), 0, s, p);
+    if (pieces <= 128 * 8) return launch_k(policy_row_kernel<T, 128, 8>, g, dim3(128), 0, s, p);
+    if (pieces <= 256 * 6) return launch_k(policy_row_kernel<T, 256, 6>, g, dim3(256), 0, s, p);
+    if (pieces <= 256 * 8) return launch_k(policy_row_kernel<T, 256, 8>, g, dim3(256), 0, s, p);
+    if (pieces <= 512 * 6) return launch_k(policy_row_kernel<T, 512, 6>, g, dim3(512), 0, s, p);
     return launch_k(policy_row_kernel<T, 512, 8>, g, dim3(512), 0, s, p);
   }
   // few rows: several CTAs each, as long as every thread has a piece

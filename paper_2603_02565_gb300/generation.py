@@ -79,6 +79,14 @@ def _stream_of(stream, index):
     return stream.cuda_stream, stream
 
 
+def _captured(on):
+    """Whether calls on stream `on` (None: the current one) are being captured."""
+    if on is None:
+        return _capturing()
+    with torch.cuda.stream(on):
+        return _capturing()
+
+
 def _like(t, on):
     """A contiguous tensor of t's shape and type, allocated for stream `on`."""
     if on is None:
@@ -223,10 +231,11 @@ class PagedKV:
             # A thread's calls on a stream run one after another and share a workspace (another thread's kernels could
             # come between the three of a call); a call that is being captured has one of its own, in the graph's memory.
             key = _thread(), handle
-            workspace = self._spaces.get(key)
-            if workspace is None or workspace.shape[0] < need or _capturing():
+            captured = _captured(on)
+            workspace = None if captured else self._spaces.get(key)
+            if workspace is None or workspace.shape[0] < need:
                 workspace = _new(q, need, on, torch.uint8)
-                if not _capturing():
+                if not captured:
                     self._spaces[key] = workspace
         elif workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be a contiguous uint8 tensor on {self.device}")

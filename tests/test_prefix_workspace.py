@@ -75,3 +75,19 @@ def test_a_graph_has_its_own():
         g.replay()
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+def test_a_captured_stream_that_is_not_the_current_one():
+    (kv, q, a, want), *_ = calls()[1:]
+    s, other = torch.cuda.Stream(), torch.cuda.Stream()
+    kv.attend(q, *a, stream=s)
+    kept = dict(kv._spaces)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s), torch.cuda.stream(other):
+        got = kv.attend(q, *a, stream=s)
+    assert kv._spaces == kept
+    for _ in range(2):
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
