@@ -25,24 +25,25 @@ def generator(example, B=3, K=5, L=20, C=50, M=40, d=128):
 
 
 def dense(gen, tokens):
-    """Hidden states of the candidates in float64: context and candidate rows in one causal sequence."""
+    """Hidden states of the candidates in float64 on the CPU: context and candidate rows in one causal sequence."""
     B, K, L, C = gen.B, gen.K, gen.L, gen.C
     S, h, kv, e = B * K, gen.heads, gen.kv_heads, gen.head_dim
     own = torch.cat([gen.begin.expand(S, 1, -1), gen.embed(tokens[:, :-1])], 1)
-    x = torch.cat([gen.context.repeat_interleave(K, 0), own], 1).double()
+    x = torch.cat([gen.context.repeat_interleave(K, 0), own], 1).cpu().double()
     n = C + L
-    c, s = gen.rope[:n, :, 0].double()[:, None], gen.rope[:n, :, 1].double()[:, None]
+    rope = gen.rope[:n].cpu().double()
+    c, s = rope[:, None, :, 0], rope[:, None, :, 1]
 
     def turn(y):
         a, b = y.chunk(2, -1)
         return torch.cat([a * c - b * s, b * c + a * s], -1)
 
     for w, mix in zip(gen.qkv, gen.mix):
-        q, k, v = (x @ w.double()).view(S, n, -1, e).split([h, kv, kv], 2)
+        q, k, v = (x @ w.cpu().double()).view(S, n, -1, e).split([h, kv, kv], 2)
         q, k = turn(q).transpose(1, 2), turn(k).transpose(1, 2).repeat_interleave(h // kv, 1)
         v = v.transpose(1, 2).repeat_interleave(h // kv, 1)
-        a = (q @ k.transpose(2, 3) * e ** -0.5 + torch.full((n, n), -torch.inf, device="cuda", dtype=torch.float64).triu(1)).softmax(-1)
-        x = x + (a @ v).transpose(1, 2).reshape(S, n, -1) @ mix.double()
+        a = (q @ k.transpose(2, 3) * e ** -0.5 + torch.full((n, n), -torch.inf, dtype=torch.float64).triu(1)).softmax(-1)
+        x = x + (a @ v).transpose(1, 2).reshape(S, n, -1) @ mix.cpu().double()
     return x[:, C:]
 
 
@@ -54,7 +55,7 @@ def test_cached_attention_is_the_dense_one(example):
     example.check_status(gen.status)
     want = dense(gen, tokens)
     # two layers of about six roundings to bf16 (2^-9 of the value in the mean square's root, at most 2^-8): well under 2^-4
-    assert (hidden.double() - want).norm() <= 2.0 ** -5 * want.norm()
+    assert (hidden.cpu().double() - want).norm() <= 2.0 ** -5 * want.norm()
     # and a token at a time writes what all rows at once read
     again = torch.log_softmax(logits.float(), -1).gather(2, tokens[..., None].long())[..., 0]
     assert (again - logp).abs().mean() <= 2.0 ** -5 * logits.float().masked_fill(logits.isinf(), 0).abs().amax()
