@@ -445,7 +445,7 @@ int fe_kv_append(const fe_append_args* args, void* stream);
  * A row that sees nothing gets out = 0 and lse = -inf.  Rows of the pages past a
  * sequence's length are never part of a result, whatever they hold (NaN too).
  *   q [n_rows, q_heads, head_dim] in the pages' type, strides as in fe_append_args;
- *   out [n_rows, q_heads, head_dim] contiguous, in the same type, 16-byte aligned, and
+ *   out [n_rows, q_heads, head_dim] contiguous, in the same type, 32-byte aligned, and
  *   no part of q;
  *   lse [n_rows, q_heads] fp32 or NULL
  *   group_start [n_groups + 1] int32, not decreasing, first 0, last n_seqs

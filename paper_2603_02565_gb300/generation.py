@@ -254,7 +254,7 @@ class PagedKV:
         """Workspace of attend for these sizes."""
         at = self._fields[5]  # (any pointer: only sizes count)
         n = _lib().fe_prefix_attention_workspace(_PREFIX.pack(
-            *self._fields, n_groups, n_seqs, n_rows, q_heads, 1, 1, 1.0, 0, at, at, at, at, at, at, at, 8, 8, at + 16, 0, 0, 0,
+            *self._fields, n_groups, n_seqs, n_rows, q_heads, 1, 1, 1.0, 0, at, at, at, at, at, at, at, 8, 8, at + 32, 0, 0, 0,
             0))
         if n == 0:
             raise FeError(_b.FE_ERR_INVALID_ARG, _lib().fe_last_error_message().decode())

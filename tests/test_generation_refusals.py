@@ -121,7 +121,7 @@ def test_append(lib, change, code):
     (dict(q_heads=0), INVALID), (dict(q_heads=3), INVALID), (dict(q_heads=4096), UNSUPPORTED),
     (dict(n_rows=1 << 30), UNSUPPORTED), (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID),
     (dict(scale=-1.0), INVALID), (dict(group_start=0), INVALID), (dict(prefix_len=0), INVALID),
-    (dict(prefix_pages=0), INVALID), (dict(seq_len=0), INVALID), (dict(out=0), INVALID), (dict(out=3 * P + 8), UNSUPPORTED),
+    (dict(prefix_pages=0), INVALID), (dict(seq_len=0), INVALID), (dict(out=0), INVALID), (dict(out=3 * P + 8), UNSUPPORTED), (dict(out=3 * P + 16), UNSUPPORTED),
     (dict(out=P), INVALID), (dict(workspace=0), INVALID), (dict(workspace=P + 128), INVALID),
 ])
 def test_attention(lib, change, code):
