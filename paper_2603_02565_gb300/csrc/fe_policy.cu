@@ -14,13 +14,14 @@
 //   longer rows        the first pass keeps 64 KB of the row in shared memory and asks L2 to
 //                      hold the rest, which the second pass reads again; gradients leave with
 //                      the lowest claim on L2.  Few rows: up to eight CTAs share one.
+//                      (Shorter rows whose gradient is aligned otherwise go this way, too.)
 // What matters is rows in different phases beside one another: three CTAs of 512 threads an SM
 // for long rows.  4096 tokens x 100000 words in bf16 (241 us at the copy
-// rate): 295 us; without the L2 hints 315, everything read twice 397 (hints alone 313), two
+// rate): 292 us; without the L2 hints 315, everything read twice 397 (hints alone 313), two
 // CTAs 322, one of 1024 threads 345.  A ring of bulk copies several rows deep in one CTA of
 // 512 threads took 440: its phases do not overlap, and clusters that share a row pay several
 // us a row (710 with the row in the registers of four CTAs).  In registers, 16384 tokens in bf16:
-// x 1000 (10 us) 21 us (28 with 128 threads, where most have nothing to do), x 8192 (79) 96,
+// x 1000 (10 us) 21 us (28 with 128 threads, where most have nothing to do), x 8192 (79) 89,
 // x 16000 (154) 171 and x 32000 (309) 342 (213 and 381 by way of shared memory).
 #include <algorithm>
 #include <cmath>
