@@ -36,3 +36,23 @@ def test_ten_thousand_sequences_of_one_row():
     rng = np.random.RandomState(6)
     S = 10000
     Batch(4, [100] * 100, rng.randint(0, 30, 100), rng.randint(1, 4, S), [1] * S, 1, 1, 32, 16, BF).check()
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_a_nan_in_a_split_unit_touches_only_the_rows_that_see_it(d):
+    """The rows of a sequence with a value that is no number are computed again after the join of 40 pieces."""
+    from paper_2603_02565_gb300 import PagedKV
+    b = Batch(8, [4], [5003], [30, 21, 9, 40], [4, 4, 4, 4], 4, 2, d, 16, BF)
+    want, lse = b.check()
+    for what, bad in (("v", float("nan")), ("v", float("inf")), ("k", float("nan"))):
+        kc, vc = b.kc.clone(), b.vc.clone()
+        (vc if what == "v" else kc)[b.own[1][18 // 16], 0, 18 % 16] = bad  # row 18 of 21: the last three query rows see it
+        out, l2 = PagedKV(kc, vc).attend(b.q, *b.args(), with_lse=True)
+        same = torch.ones(16, 4, dtype=torch.bool, device="cuda")
+        same[5:8, :2] = False  # sequence 1's rows see its rows 0 .. 17, .. 18, .. 19, .. 20; its key head 0 has query heads 0, 1
+        # (the row before the bad one is in a recomputed sequence: another order of sums, the same numbers rounded)
+        again = torch.zeros_like(same)
+        again[4, :2] = True
+        assert torch.equal(out[same & ~again], want[same & ~again])
+        assert torch.allclose(out[again].float(), want[again].float(), rtol=2.0 ** -6, atol=2.0 ** -7)
+        assert not torch.isfinite(out[~same]).any()
