@@ -68,9 +68,11 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p) 
   const long long w = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   const int t = (int)(w / p.parts), part = (int)(w % p.parts);
   if (t >= p.n_rows) return;
-  // the row's sequence: row t's own when every sequence has one new row
+  // the row's sequence: t's own when every sequence has one new row (as many rows as sequences, but t in another one
+  // where some have none and others several)
   int s = t;
-  if (p.n_rows != p.n_seqs || __ldg(p.row_start + t) != t) s = warp_find_row(p.row_start, p.n_seqs, t);
+  if (p.n_rows != p.n_seqs || __ldg(p.row_start + t) != t || __ldg(p.row_start + t + 1) <= t)
+    s = warp_find_row(p.row_start, p.n_seqs, t);
   const int j = t - __ldg(p.row_start + s);
   const long long c = (long long)__ldg(p.first + s) + j;
   const long long pos = c + (p.shift ? __ldg(p.shift + s) : 0);
