@@ -495,7 +495,7 @@ int fe_prefix_attention(const fe_prefix_args* args, void* stream);
  *          term); loss [1], terms, logp, lse, coef [rows]: fp32
  * A token of weight 0 takes no part: its logits are not read, its outputs and its
  * gradient are 0.  A token outside [0, vocab) gets NaN throughout: FE_ST_INDEX.
- * Logits of -inf have probability 0.
+ * Logits of -inf have probability 0; a NaN among a token's makes all of its outputs NaN.
  * fe_policy_loss_backward writes grad alone, from the lse and coef of an earlier call
  * (weights and the tokens' order unchanged) times *upstream (a device float, NULL: 1).
  * Errors: FE_ERR_INVALID_ARG, FE_ERR_UNSUPPORTED, FE_ERR_CUDA.

@@ -52,9 +52,10 @@ struct MaxSum {
   float m, s;
 };
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
-// a sum against maximum m0 as one against m >= m0
+// a sum against maximum m0 as one against m >= m0 (m0 -inf: a sum of nothing, 0, or one that a NaN has come into, which
+// a maximum does not show)
 __device__ __forceinline__ float rebase(float s, float m0, float m, float c) {
-  return m0 == -INFINITY ? 0.f : s * ex2_approx((m0 - m) * c);
+  return m0 == -INFINITY ? s : s * ex2_approx((m0 - m) * c);
 }
 __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c) {
   const float m = fmaxf(a.m, b.m);
@@ -103,7 +104,7 @@ __device__ __forceinline__ Token token_of(const PolicyParams& p, int t) {
 __device__ __forceinline__ float row_outputs(const PolicyParams& p, int t, const Token& k, float xy, MaxSum v, bool write) {
   const float l2 = log2f(v.s);
   float logp = ((xy - v.m) * p.c - l2) * kLn2, lse = v.m * p.inv_t + l2 * kLn2;
-  if (v.m == -INFINITY) lse = -INFINITY, logp = NAN;
+  if (v.m == -INFINITY) lse = v.s == v.s ? -INFINITY : NAN, logp = NAN;
   if (!k.valid(p.vocab)) logp = NAN;
   const float r = p.old_logp ? expf(logp - k.old) : 1.f;
   const float plain = r * k.adv, clipped = fminf(fmaxf(r, 1.f - p.lo), 1.f + p.hi) * k.adv;
