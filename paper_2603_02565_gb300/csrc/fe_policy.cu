@@ -105,7 +105,7 @@ __device__ __forceinline__ float row_outputs(const PolicyParams& p, int t, const
   const float l2 = log2f(v.s);
   float logp = ((xy - v.m) * p.c - l2) * kLn2, lse = v.m * p.inv_t + l2 * kLn2;
   if (v.m == -INFINITY) lse = v.s == v.s ? -INFINITY : NAN, logp = NAN;
-  if (!k.valid(p.vocab)) logp = NAN;
+  if (!k.valid(p.vocab)) logp = lse = NAN;
   const float r = p.old_logp ? expf(logp - k.old) : 1.f;
   const float plain = r * k.adv, clipped = fminf(fmaxf(r, 1.f - p.lo), 1.f + p.hi) * k.adv;
   float term = plain <= clipped ? -plain : -clipped, coef = plain <= clipped ? -plain : 0.f;

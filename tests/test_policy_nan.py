@@ -53,3 +53,22 @@ def test_rows_with_nan(T, V, where, dtype, grad):
     assert torch.isnan(r.loss)
     if grad:
         assert torch.isnan(r.grad[bad]).all() and torch.equal(r.grad[~bad], clean.grad[~bad])
+
+
+@pytest.mark.parametrize("T,V", [(5, 64), (5, 40000), (400, 40000)])
+@pytest.mark.parametrize("token", [-1, "V", 2 ** 31 - 1])
+def test_an_invalid_token_leaves_no_number(T, V, token):
+    """Its lse too: nothing of such a row is to be used."""
+    from paper_2603_02565_gb300 import policy_loss
+    logits, y, adv, w, old, _ = make(V, 5, V, torch.bfloat16)
+    n = T // 5
+    logits = logits.repeat(n, 1)
+    y, adv, w, old = (np.tile(a, n) for a in (y, adv, w, old))
+    y[2] = V if token == "V" else token
+    status = dev([0], torch.int32)
+    r = policy_loss(logits, dev(y, torch.int32), dev(adv), dev(w), old_logp=dev(old), status=status)
+    assert status.item() == 1
+    for name in ("logp", "lse", "terms", "coef"):
+        got = torch.isnan(getattr(r, name))
+        assert got[2] and got.sum() == 1, name
+    assert torch.isnan(r.loss) and torch.isnan(r.grad[2]).all() and torch.isnan(r.grad).any(1).sum() == 1
