@@ -53,13 +53,12 @@ namespace fe {
 namespace {
 
 constexpr int kUnitRows = 128, kTileKeys = 128, kSlot = 16, kSlots = kTileKeys / kSlot;
-constexpr int kListed = 1 << 16;  // rows to compute again that the list holds
 constexpr int kDirty = 3, kUnitsAhead = 8;
 
 struct PlanHead {
   int status;   // ST_ bits of this call
   int bad;      // the row or group offsets are not what they must be: all rows NaN
-  int listed;   // rows to compute again (more than kListed: all rows are looked at)
+  int listed;   // rows to compute again
 };
 // A split unit: its rows, and the CTAs that have its pieces (count 0: none).  While the schedule runs, count is its
 // tiles, the first of them tile.
@@ -86,7 +85,7 @@ struct PrefixParams {
   int* cost;           // [max_tiles] key tiles of a row tile (one head), at least 1
   long long* before;   // [max_tiles + 1] key tiles of one head before a row tile
   SplitRec* recs;      // [ctas][2] the split unit that a CTA begins in the middle of, the one it ends in the middle of
-  int* list;           // [kListed]
+  int* list;           // [n_rows hq] rows of the output to compute again: those that a CTA has whole and that are NaN
   float* part_o;       // [ctas][2][kUnitRows][D]
   float2* part_ml;     // [ctas][2][kUnitRows] maximum (log2 units) and sum
 };
@@ -1225,10 +1224,7 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
       }
       tc_fence_before();
       if (store && direct) {
-        if (!(l == l)) {
-          const int at = atomicAdd(&p.head->listed, 1);
-          if (at < kListed) p.list[at] = ri.out;
-        }
+        if (!(l == l)) p.list[atomicAdd(&p.head->listed, 1)] = ri.out;
         if (p.lse) p.lse[ri.out] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147180559945309f;
       } else if (store) {
         p.part_ml[slot] = make_float2(m, l);
@@ -1403,17 +1399,9 @@ __global__ void __launch_bounds__(256) prefix_finish_kernel(const PrefixParams p
       put(r, m, l, o);
     }
   }
+  // (in any order: a row depends on nothing but its keys)
   const int listed = p.head->listed;
-  if (listed <= kListed) {
-    for (long long i = w0; i < listed; i += nw) row_by_keys<T, D>(p, p.list[i], sq[wp]);
-  } else {
-    for (long long w = w0; w < rows; w += nw) {
-      const T* out = reinterpret_cast<const T*>(p.out) + w * D;
-      float check = 0.f;
-      for (int i = lane; i < D; i += 32) check = fmaf(Elem<T>::get(out[i]), 0.f, check);
-      if (__any_sync(0xffffffffu, !(check == 0.f))) row_by_keys<T, D>(p, w, sq[wp]);
-    }
-  }
+  for (long long i = w0; i < listed; i += nw) row_by_keys<T, D>(p, p.list[i], sq[wp]);
 }
 int check_prefix(const fe_prefix_args* a) {
   if (!a) return fail(FE_ERR_INVALID_ARG, "null arguments");
@@ -1457,7 +1445,7 @@ Layout layout(const fe_prefix_args* a, int ctas, int max_tiles) {
   w.cost = take(4 * (size_t)max_tiles);
   w.before = take(8 * ((size_t)max_tiles + 1));
   w.recs = take(sizeof(SplitRec) * 2 * ctas);
-  w.list = take(4 * (size_t)kListed);
+  w.list = take(4 * (size_t)a->n_rows * a->q_heads);
   w.part_o = take((size_t)ctas * 2 * kUnitRows * a->kv.head_dim * 4);
   w.part_ml = take((size_t)ctas * 2 * kUnitRows * 8);
   w.bytes = at;
