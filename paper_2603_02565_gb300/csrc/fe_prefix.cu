@@ -87,7 +87,7 @@ struct PrefixParams {
   SplitRec* recs;      // [ctas][2] the split unit that a CTA begins in the middle of, the one it ends in the middle of
   int* list;           // [n_rows hq] rows of the output to compute again: those that a CTA has whole and that are NaN
   float* part_o;       // [ctas][2][kUnitRows][D]
-  float2* part_ml;     // [ctas][2][kUnitRows] maximum (log2 units) and sum
+  float2* part_ml;     // [ctas][2][kUnitRows] reference (about the maximum, log2 units) and sum of the weights
 };
 
 // The sequence's own rows that row j of its n sees, and whether its length is one
@@ -1077,8 +1077,12 @@ __global__ void __launch_bounds__(PrefixCfg<D>::kThreads, 2)
             }
             }
           }
-          mx *= sc;
-          constexpr float kSlack = 8.f;
+          // Weights are 2^(x - m) in the values' type, which the product wants of both its operands (the sum keeps them
+          // in fp32): rounded once, by u of each.  m is kLift below the row's maximum and may lag kSlack more, which
+          // makes weights of up to 2^15 in f16.  Its smallest numbers would otherwise drop weights below 2^-25 of
+          // the largest, which thousands of keys may have; so it is 2^-32.  bf16 has fp32's range.
+          constexpr float kSlack = 8.f, kLift = std::is_same<T, __half>::value ? 7.f : 0.f;
+          mx = fmaf(mx, sc, -kLift);
           if (mine == 0) {
             m = mx;
           } else {
