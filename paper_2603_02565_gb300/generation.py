@@ -21,6 +21,7 @@ from __future__ import annotations
 import math
 import struct
 import threading
+import weakref
 
 import torch
 
@@ -67,7 +68,6 @@ _current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: to
 
 
 _capturing = torch.cuda.is_current_stream_capturing
-_thread = threading.get_ident
 
 
 def _stream_of(stream, index):
@@ -85,6 +85,23 @@ def _captured(on):
         return _capturing()
     with torch.cuda.stream(on):
         return _capturing()
+
+
+class _Kept(threading.local):
+    """A PagedKV's workspaces by stream, each thread's its own: they go with the thread."""
+
+    def __init__(self):
+        self.spaces = {}
+
+
+class _Shared(threading.local):
+    """The same by device and stream over all PagedKV, as long as one of them keeps them: a model's layers share one."""
+
+    def __init__(self):
+        self.spaces = weakref.WeakValueDictionary()
+
+
+_shared = _Shared()
 
 
 def _like(t, on):
@@ -146,8 +163,7 @@ class PagedKV:
         self._fields = (_TYPES[k.dtype], self.n_pages, self.page_rows, self.kv_heads, self.head_dim, k.data_ptr(),
                         v.data_ptr())
         self._scale = 1.0 / math.sqrt(self.head_dim)
-        self._need = {}  # workspace bytes by sizes
-        self._spaces = {}  # a workspace by thread and stream
+        self._kept = _Kept()
 
     @classmethod
     def empty(cls, n_pages, page_rows, kv_heads, head_dim, dtype=torch.bfloat16, device="cuda"):
@@ -214,8 +230,9 @@ class PagedKV:
         that sequence s holds in pages[s]; each sees the rows up to itself, and the prefix_lengths[g] rows in
         prefix_pages[g] of the group g with group_start[g] <= s < group_start[g + 1].  scale: 1 / sqrt(head_dim)
         unless given.  Returns out [rows, q_heads, head_dim], with with_lse (out, lse [rows, q_heads] fp32); a
-        row that sees nothing gets 0 and -inf.  workspace: a uint8 tensor to use instead of the one that this object
-        keeps for each thread and stream (workspace_bytes says how much); not to be shared by calls that may overlap."""
+        row that sees nothing gets 0 and -inf.  workspace: a uint8 tensor to use instead of the one that is kept for
+        each thread and stream, for all PagedKV of a device (workspace_bytes says how much); not to be shared by calls
+        that may overlap."""
         dev = self._index
         G, S, T = prefix_lengths.shape[0], lengths.shape[0], q.shape[0]
         qp, hq, q_row, q_head = self._rows("q", q, T)
@@ -225,30 +242,42 @@ class PagedKV:
         out = _like(q, on) if out is None else self._out("out", out, q)
         lse = _new(q, (T, hq), on, torch.float32) if with_lse else None
         if workspace is None:
-            need = self._need.get((G, S, T, hq))
-            if need is None:
-                need = self._need[G, S, T, hq] = self.workspace_bytes(G, S, T, hq)
             # A thread's calls on a stream run one after another and share a workspace (another thread's kernels could
             # come between the three of a call); a call that is being captured has one of its own, in the graph's memory.
-            key = _thread(), handle
-            captured = _captured(on)
-            workspace = None if captured else self._spaces.get(key)
-            if workspace is None or workspace.shape[0] < need:
-                workspace = _new(q, need, on, torch.uint8)
-                if not captured:
-                    self._spaces[key] = workspace
+            keep = None if _captured(on) else handle
+            workspace = self._spaces.get(keep)
+            if workspace is None:
+                workspace = self._workspace(keep, G, S, T, hq, q, on)
         elif workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be a contiguous uint8 tensor on {self.device}")
         else:
-            need = workspace.numel()
-        rc = _lib().fe_prefix_attention(_PREFIX.pack(
+            keep = None
+        fields = (
             *self._fields, G, S, T, hq, pre_cols, cols, self._scale if scale is None else scale, 0,
             _i32("group_start", group_start, G + 1, dev), _i32("prefix_lengths", prefix_lengths, G, dev), pre_table,
             _i32("row_start", row_start, S + 1, dev), _i32("lengths", lengths, S, dev), table, qp, q_row, q_head,
-            out.data_ptr(), 0 if lse is None else lse.data_ptr(), workspace.data_ptr(), need, _status(status, dev)), handle)
+            out.data_ptr(), 0 if lse is None else lse.data_ptr())
+        status = _status(status, dev)
+        rc = _lib().fe_prefix_attention(_PREFIX.pack(*fields, workspace.data_ptr(), workspace.numel(), status), handle)
+        if rc == _b.FE_ERR_WORKSPACE and keep is not None:  # (nothing has been enqueued)
+            workspace = self._workspace(keep, G, S, T, hq, q, on)
+            rc = _lib().fe_prefix_attention(_PREFIX.pack(*fields, workspace.data_ptr(), workspace.numel(), status), handle)
         if rc:
             _check(rc)
         return (out, lse) if with_lse else out
+
+    _spaces = property(lambda self: self._kept.spaces)  # this thread's workspaces by stream handle
+
+    def _workspace(self, keep, G, S, T, hq, q, on):
+        """A workspace for a call of these sizes, to be kept for the stream with handle `keep` unless that is None."""
+        need = self.workspace_bytes(G, S, T, hq)
+        if keep is None:
+            return _new(q, need, on, torch.uint8)
+        workspace = _shared.spaces.get((self._index, keep))
+        if workspace is None or workspace.numel() < need:
+            workspace = _shared.spaces[self._index, keep] = _new(q, need, on, torch.uint8)
+        self._spaces[keep] = workspace
+        return workspace
 
     def workspace_bytes(self, n_groups: int, n_seqs: int, n_rows: int, q_heads: int) -> int:
         """Workspace of attend for these sizes."""
