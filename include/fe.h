@@ -369,7 +369,8 @@ int fe_debug_wait_probe(fe_ctx* ctx, uint32_t limit_us, void* stream);
  * allocate nothing, keep nothing between calls, and enqueue on `stream`
  * (a cudaStream_t) without waiting; calls on different streams are
  * independent as long as their outputs, pages written and workspaces differ.
- * They can be captured in a CUDA graph.  Every pointer is a device pointer;
+ * They can be captured in a CUDA graph.  The calling thread's current device must
+ * be that of `stream` and of the pointers, which are all device pointers;
  * arguments the host can see are checked before anything is enqueued, indices
  * in device memory by the kernels, which OR FE_ST_INDEX into *status (a device
  * word that the caller clears; NULL: not reported) and confine the damage to the
