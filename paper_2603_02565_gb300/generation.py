@@ -332,15 +332,14 @@ def _logits(logits):
 
 
 def _grad(logits, row, grad, on):
-    """(tensor, row stride) of the gradient: a new one has its rows as far apart as the logits', the same alignment."""
-    if grad is None:
-        if logits.is_contiguous():
-            return _like(logits, on), row
-        if on is None:
-            return torch.empty_strided(logits.shape, (row, 1), dtype=logits.dtype, device=logits.device), row
-        with torch.cuda.stream(on):
-            return torch.empty_strided(logits.shape, (row, 1), dtype=logits.dtype, device=logits.device), row
+    """(tensor, row stride) of the gradient: a new one has its rows as far apart as the logits', and as far off a
+    16-byte boundary (so they leave the kernels in whole pieces)."""
     T, V = logits.shape
+    if grad is None:
+        off = logits.data_ptr() % 16 // logits.element_size()
+        if off == 0 and logits.is_contiguous():
+            return _like(logits, on), row
+        return _new(logits, off + max(0, (T - 1) * row + V), on).as_strided((T, V), (row, 1), off), row
     if grad.shape != logits.shape or grad.dtype is not logits.dtype or grad.get_device() != logits.get_device() or (
             grad.stride(1) != 1 and V > 1):
         raise ValueError("grad must have the logits' shape, type and device, and contiguous rows")
