@@ -22,6 +22,7 @@ from __future__ import annotations
 import math
 import struct
 import threading
+import warnings
 import weakref
 
 import torch
@@ -78,6 +79,13 @@ def _on_device(index, entry, *args):
         return entry(*args)
     with torch.cuda.device(index):
         return entry(*args)
+
+
+def _cut_off(name):
+    """Called where tensors of a call require a gradient."""
+    if torch.is_grad_enabled():
+        warnings.warn(f"{name} has no backward: its results are cut off from tensors that require a gradient (call it "
+                      "under torch.no_grad(), or with detached tensors)", stacklevel=3)
 
 
 def _stream_of(stream, index):
@@ -205,11 +213,13 @@ class PagedKV:
         row_start[s] .. row_start[s + 1] - 1 go to rows first[s], first[s] + 1, ... of sequence s, whose pages are
         pages[s].  With rope ([positions, rot_dim / 2, 2] fp32, see rotary_table) keys, and the queries
         q [rows, q_heads, head_dim] when given, are rotated at position shift[s] + first[s] + j; pairs: "half"
-        or "interleaved".  Returns the rotated queries (q_out, contiguous), or None without q."""
+        or "interleaved".  Returns the rotated queries (q_out, contiguous), or None without q.  There is no backward."""
         dev = self._index
         S, T = first.shape[0], k.shape[0]
         kp, _, k_row, k_head = self._rows("k", k, T, self.kv_heads)
         vp, _, v_row, v_head = self._rows("v", v, T, self.kv_heads)
+        if k.requires_grad or v.requires_grad or (q is not None and q.requires_grad):
+            _cut_off("append")
         if pairs not in _PAIRS:
             raise ValueError("pairs must be 'half' or 'interleaved'")
         rope_p = rope_rows = rot = 0
@@ -244,10 +254,12 @@ class PagedKV:
         unless given.  Returns out [rows, q_heads, head_dim], with with_lse (out, lse [rows, q_heads] fp32); a
         row that sees nothing gets 0 and -inf.  workspace: a uint8 tensor to use instead of the one that is kept for
         each thread and stream, for all PagedKV of a device (workspace_bytes says how much); not to be shared by calls
-        that may overlap."""
+        that may overlap.  There is no backward."""
         dev = self._index
         G, S, T = prefix_lengths.shape[0], lengths.shape[0], q.shape[0]
         qp, hq, q_row, q_head = self._rows("q", q, T)
+        if q.requires_grad or self.k.requires_grad or self.v.requires_grad:
+            _cut_off("attend")
         table, cols = _table("pages", pages, S, dev)
         pre_table, pre_cols = _table("prefix_pages", prefix_pages, G, dev)
         handle, on = _stream_of(stream, dev)
