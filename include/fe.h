@@ -378,8 +378,9 @@ int fe_debug_wait_probe(fe_ctx* ctx, uint32_t limit_us, void* stream);
  * ---------------------------------------------------------------------------
  */
 
-/* Bits of a device status word. */
-enum { FE_ST_INDEX = 1, FE_ST_NUMERIC = 2, FE_ST_TIMEOUT = 4 };
+/* Bits of a device status word: an index or length out of range; a bounded wait of
+ * fe_prefix_attention gave up (its results are invalid). */
+enum { FE_ST_INDEX = 1, FE_ST_TIMEOUT = 4 };
 
 /* The pairs that a rotation by position turns: (x_i, x_{i + rot/2}) or (x_2i, x_{2i+1}). */
 enum { FE_PAIRS_HALF = 0, FE_PAIRS_INTERLEAVED = 1 };
@@ -453,7 +454,8 @@ int fe_kv_append(const fe_append_args* args, void* stream);
  *   prefix_pages [n_groups, prefix_cols], pages [n_seqs, page_cols] int32
  * Softmax statistics and accumulators are fp32.  The result does not depend on the
  * timing of the run.  A page entry outside [0, n_pages), or a length that is negative
- * or does not fit the page table, makes the rows that see it NaN: FE_ST_INDEX.
+ * or does not fit the page table, makes the rows that see it NaN: FE_ST_INDEX.  When a
+ * bounded wait of its kernels gives up, all results are invalid: FE_ST_TIMEOUT.
  * The workspace (fe_prefix_attention_workspace bytes for the same args, 256-byte
  * aligned) is the call's own until it has run; what it holds before is of no
  * importance.  fe_prefix_attention_workspace returns 0 for arguments that are refused.

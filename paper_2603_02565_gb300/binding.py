@@ -28,7 +28,6 @@ FE_IO_BF16 = 0
 FE_IO_F32 = 1
 FE_IO_F16 = 2
 FE_ST_INDEX = 1
-FE_ST_NUMERIC = 2
 FE_ST_TIMEOUT = 4
 
 EXPORTS = ["fe_weight_count", "fe_init", "fe_reserve", "fe_evaluate", "fe_evaluate_async", "fe_last_status",

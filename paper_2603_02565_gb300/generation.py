@@ -54,8 +54,6 @@ def check_status(status) -> None:
         raise FeError(_b.FE_ERR_TIMEOUT, "device-side wait timed out")
     if st & _b.FE_ST_INDEX:
         raise FeError(_b.FE_ERR_INDEX, "an index or length in device memory is out of range")
-    if st & _b.FE_ST_NUMERIC:
-        raise FeError(_b.FE_ERR_NUMERIC, "NaN")
 
 
 def rotary_table(n_positions: int, rot_dim: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
