@@ -57,7 +57,7 @@ __device__ __forceinline__ void turn(uint4& a, uint4& b, const float* cs, bool h
 }
 
 constexpr int kThreads = 256;
-constexpr long long kWarps = 32 * 152;  // that the SMs hold (64 registers a thread)
+constexpr int kWarps = 32;  // that an SM holds (64 registers a thread)
 
 template <typename T, int D, bool HALF>
 __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p) {
@@ -203,11 +203,15 @@ extern "C" int fe_kv_append(const fe_append_args* a, void* stream) {
   p.rope_rows = a->rope_rows;
   p.rot = a->rope ? a->rot_dim : 0;
   const int heads = 512 / a->kv.head_dim, steps = (p.hq + 2 * p.hkv + heads - 1) / heads;  // of a warp over a row
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return fail_cuda(e, "fe_kv_append");
   p.parts = 1;
-  while (2 * p.parts <= steps && 2LL * p.n_rows * p.parts <= kWarps) p.parts *= 2;
+  while (2 * p.parts <= steps && 2LL * p.n_rows * p.parts <= (long long)kWarps * sms) p.parts *= 2;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool half = a->pairs == FE_PAIRS_HALF;
-  const cudaError_t e = a->kv.dtype == FE_IO_BF16 ? append_dim<__nv_bfloat16>(p, a->kv.head_dim, half, s)
+  e = a->kv.dtype == FE_IO_BF16 ? append_dim<__nv_bfloat16>(p, a->kv.head_dim, half, s)
                                                   : append_dim<__half>(p, a->kv.head_dim, half, s);
   return e == cudaSuccess ? FE_OK : fail_cuda(e, "fe_kv_append");
 }
