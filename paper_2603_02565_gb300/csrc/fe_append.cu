@@ -14,6 +14,8 @@
 // row each of 64 / 256 / 1024 sequences take 3.8 / 4.3 / 7.2 us (7.3 / 7.5 / 8.0 unsplit; the
 // launch alone is 3), of 4096 18.4 (24 with more parts than that; 14.8 at the copy rate).
 // 37 prompts of up to 8000 rows: 590 us, 6.4 TB/s of 6.8 measured for a copy.
+#include <atomic>
+
 #include "fe_ops.cuh"
 
 namespace fe {
@@ -151,6 +153,18 @@ cudaError_t append_dim(const AppendParams& p, int d, bool half, cudaStream_t s) 
   return d == 32 ? append_go<T, 32>(p, half, s) : d == 64 ? append_go<T, 64>(p, half, s) : append_go<T, 128>(p, half, s);
 }
 
+// SMs of the current device, asked for once
+cudaError_t device_sms(int* sms) {
+  static std::atomic<int> known[64];
+  int d = 0;
+  cudaError_t e = cudaGetDevice(&d);
+  if (e != cudaSuccess) return e;
+  if (d < 64 && (*sms = known[d].load(std::memory_order_relaxed)) > 0) return e;
+  e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, d);
+  if (e == cudaSuccess && d < 64) known[d].store(*sms, std::memory_order_relaxed);
+  return e;
+}
+
 bool bad_strides(const void* x, int64_t row, int64_t head) { return misaligned(x, 16) || row % 8 != 0 || head % 8 != 0; }
 
 }  // namespace
@@ -203,15 +217,14 @@ extern "C" int fe_kv_append(const fe_append_args* a, void* stream) {
   p.rope_rows = a->rope_rows;
   p.rot = a->rope ? a->rot_dim : 0;
   const int heads = 512 / a->kv.head_dim, steps = (p.hq + 2 * p.hkv + heads - 1) / heads;  // of a warp over a row
-  int dev = 0, sms = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  int sms = 0;
+  cudaError_t e = device_sms(&sms);
   if (e != cudaSuccess) return fail_cuda(e, "fe_kv_append");
   p.parts = 1;
   while (2 * p.parts <= steps && 2LL * p.n_rows * p.parts <= (long long)kWarps * sms) p.parts *= 2;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool half = a->pairs == FE_PAIRS_HALF;
   e = a->kv.dtype == FE_IO_BF16 ? append_dim<__nv_bfloat16>(p, a->kv.head_dim, half, s)
-                                                  : append_dim<__half>(p, a->kv.head_dim, half, s);
+                                : append_dim<__half>(p, a->kv.head_dim, half, s);
   return e == cudaSuccess ? FE_OK : fail_cuda(e, "fe_kv_append");
 }
