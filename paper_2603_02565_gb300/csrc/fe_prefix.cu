@@ -1404,8 +1404,9 @@ __global__ void __launch_bounds__(256) prefix_finish_kernel(const PrefixParams p
     }
   }
   // (in any order: a row depends on nothing but its keys)
-  const int listed = p.head->listed;
-  for (long long i = w0; i < listed; i += nw) row_by_keys<T, D>(p, p.list[i], sq[wp]);
+  const uint32_t listed = p.head->listed, step = gridDim.x * gridDim.y * 8;
+#pragma unroll 1
+  for (uint32_t i = (blockIdx.y * gridDim.x + blockIdx.x) * 8 + wp; i < listed; i += step) row_by_keys<T, D>(p, p.list[i], sq[wp]);
 }
 int check_prefix(const fe_prefix_args* a) {
   if (!a) return fail(FE_ERR_INVALID_ARG, "null arguments");
