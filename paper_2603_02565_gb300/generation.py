@@ -71,12 +71,16 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 _capturing = torch.cuda.is_current_stream_capturing
 
 
-def _on_device(index, entry, *args):
-    """entry(*args) with CUDA device `index` current: the library's calls and the current stream's state are that device's."""
+def _on_device(index, entry):
+    """`entry`, called with CUDA device `index` current: the library's calls, and what torch says of the current stream,
+    are that device's."""
     if index == _current_device():
-        return entry(*args)
-    with torch.cuda.device(index):
-        return entry(*args)
+        return entry
+
+    def call(*args):
+        with torch.cuda.device(index):
+            return entry(*args)
+    return call
 
 
 def _cut_off(name):
@@ -100,7 +104,7 @@ def _stream_of(stream, index):
 def _captured(on, index):
     """Whether calls on stream `on` (None: the current one of device `index`) are being captured."""
     if on is None:
-        return _on_device(index, _capturing)
+        return _on_device(index, _capturing)()
     with torch.cuda.stream(on):
         return _capturing()
 
@@ -234,7 +238,7 @@ class PagedKV:
             qp, hq, q_row, q_head = self._rows("q", q, T)
             q_out = _like(q, on) if q_out is None else self._out("q_out", q_out, q)
             out_p = q_out.data_ptr()
-        rc = _on_device(dev, _lib().fe_kv_append, _APPEND.pack(
+        rc = _on_device(dev, _lib().fe_kv_append)(_APPEND.pack(
             *self._fields, S, T, cols, hq, rope_rows, rot, _PAIRS[pairs], 0, _i32("row_start", row_start, S + 1, dev),
             _i32("first", first, S, dev), 0 if shift is None else _i32("shift", shift, S, dev), table, kp, vp, qp, k_row,
             k_head, v_row, v_head, q_row, q_head, out_p, rope_p, _status(status, dev)), handle)
@@ -267,25 +271,27 @@ class PagedKV:
             # A thread's calls on a stream run one after another and share a workspace (another thread's kernels could
             # come between the three of a call); a call that is being captured has one of its own, in the graph's memory.
             keep = None if _captured(on, dev) else handle
-            workspace = self._spaces.get(keep)
+            workspace = self._kept.spaces.get(keep)
             if workspace is None:
                 workspace = self._workspace(keep, G, S, T, hq, q, on)
         elif workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be a contiguous uint8 tensor on {self.device}")
         else:
             keep = None
-        fields = (
-            *self._fields, G, S, T, hq, pre_cols, cols, self._scale if scale is None else scale, 0,
-            _i32("group_start", group_start, G + 1, dev), _i32("prefix_lengths", prefix_lengths, G, dev), pre_table,
-            _i32("row_start", row_start, S + 1, dev), _i32("lengths", lengths, S, dev), table, qp, q_row, q_head,
-            out.data_ptr(), 0 if lse is None else lse.data_ptr())
-        status, entry = _status(status, dev), _lib().fe_prefix_attention
-        rc = _on_device(dev, entry, _PREFIX.pack(*fields, workspace.data_ptr(), workspace.numel(), status), handle)
-        if rc == _b.FE_ERR_WORKSPACE and keep is not None:  # (nothing has been enqueued)
-            workspace = self._workspace(keep, G, S, T, hq, q, on)
-            rc = _on_device(dev, entry, _PREFIX.pack(*fields, workspace.data_ptr(), workspace.numel(), status), handle)
-        if rc:
-            _check(rc)
+        entry = _on_device(dev, _lib().fe_prefix_attention)
+        while True:
+            rc = entry(_PREFIX.pack(
+                *self._fields, G, S, T, hq, pre_cols, cols, self._scale if scale is None else scale, 0,
+                _i32("group_start", group_start, G + 1, dev), _i32("prefix_lengths", prefix_lengths, G, dev), pre_table,
+                _i32("row_start", row_start, S + 1, dev), _i32("lengths", lengths, S, dev), table, qp, q_row, q_head,
+                out.data_ptr(), 0 if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                _status(status, dev)), handle)
+            if rc == 0:
+                break
+            if rc != _b.FE_ERR_WORKSPACE or keep is None:
+                _check(rc)
+            # the kept workspace is one of smaller calls (nothing has been enqueued)
+            workspace, keep = self._workspace(keep, G, S, T, hq, q, on), None
         return (out, lse) if with_lse else out
 
     _spaces = property(lambda self: self._kept.spaces)  # this thread's workspaces by stream handle
@@ -304,7 +310,7 @@ class PagedKV:
     def workspace_bytes(self, n_groups: int, n_seqs: int, n_rows: int, q_heads: int) -> int:
         """Workspace of attend for these sizes."""
         at = self._fields[5]  # (any pointer: only sizes count)
-        n = _on_device(self._index, _lib().fe_prefix_attention_workspace, _PREFIX.pack(
+        n = _on_device(self._index, _lib().fe_prefix_attention_workspace)(_PREFIX.pack(
             *self._fields, n_groups, n_seqs, n_rows, q_heads, 1, 1, 1.0, 0, at, at, at, at, at, at, at, 8, 8, at + 32, 0, 0, 0,
             0))
         if n == 0:
@@ -374,7 +380,7 @@ def policy_loss(logits, tokens, advantages, weights=None, *, old_logp=None, ref_
         grad = None
     stats = _new(logits, 4 * T + 1, on, torch.float32)
     at, n = stats.data_ptr(), 4 * T
-    rc = _on_device(dev, _lib().fe_policy_loss, _POLICY.pack(
+    rc = _on_device(dev, _lib().fe_policy_loss)(_POLICY.pack(
         dtype, T, V, clip[0], clip[1], beta, temperature, grad_scale, logits.data_ptr(), row, grad_row,
         _i32("tokens", tokens, T, dev), _f32("advantages", advantages, T, dev), _f32("weights", weights, T, dev),
         _f32("old_logp", old_logp, T, dev), _f32("ref_logp", ref_logp, T, dev), at, at + 4, at + 4 + n, at + 4 + 2 * n,
@@ -391,7 +397,7 @@ def policy_loss_backward(logits, tokens, result: PolicyLoss, weights=None, *, up
     T, V, dtype, dev, row = _logits(logits)
     handle, on = _stream_of(stream, dev)
     grad, grad_row = _grad(logits, row, grad, on)
-    rc = _on_device(dev, _lib().fe_policy_loss_backward, _POLICY.pack(
+    rc = _on_device(dev, _lib().fe_policy_loss_backward)(_POLICY.pack(
         dtype, T, V, 0.0, 0.0, 0.0, temperature, grad_scale, logits.data_ptr(), row, grad_row,
         _i32("tokens", tokens, T, dev), 0, _f32("weights", weights, T, dev), 0, 0, 0, 0, 0,
         _f32("lse", result.lse, T, dev), _f32("coef", result.coef, T, dev), grad.data_ptr(), _status(status, dev)),
