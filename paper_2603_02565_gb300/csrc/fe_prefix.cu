@@ -32,11 +32,12 @@
 //   2 groups x 8 sequences, up to 256 rows each, prefixes of 8192, the same heads:
 //     411 us, 1130 TFLOP/s (cuBLAS 1895).  The products take half of the time, the chain
 //     scores - maximum - weights - product of two CTAs the rest;
-//   256 groups x 50 sequences, a token each, prefixes of 256, 4 heads of 32: 87 us (bytes
-//     alone 9): a tile's steps again, each of few instructions per byte;
+//   256 groups x 50 sequences, a token each, prefixes of 256, 4 heads of 32: 88 us (bytes
+//     alone 9): a tile's steps again, for nine tiles a unit of which seven are own keys, one to six of
+//     them in a slot of 16;
 //   1 group x 4 sequences, prefix of 300, 8 heads of 64: 17 us, of which three launches 8.
-// A tile of 128 keys costs each row 128 exponentials, at sixteen a clock and SM 1.1 us for the
-// tiles of both CTAs: no head dimension of 32 or 64 can go below that.
+// A tile of 128 keys that a row sees whole costs it 128 exponentials, at sixteen a clock and SM 1.1 us
+// for the tiles of both CTAs (a row that sees one slot of a tile: 16).
 //
 // 0 x NaN is NaN, so a value that is no number spoils rows that give it no weight.  The
 // values' warp clears the value rows past a sequence's end, whatever the pages hold there,
