@@ -613,7 +613,8 @@ int fe_nibble_attention(const fe_nibble_attention_args* args, void* stream);
  *   the first i with sum_{k <= i} w_k > sample[s] sum_k w_k
  *   accepted[s] = drafts accepted
  *   out[t] = the accepted drafts, then the token drawn, then -1
- * Comparisons are exact; sums hold each w to 2^-46.
+ * Comparisons are exact; sums hold each w to 2^-46, or where p - q does not fit a 32-bit float, to
+ * 1.25 times that.  A row whose sum is 2^17 or more counts as one that has other values.
  *   target, draft [n_rows, vocab] bf16, f16 or fp32, rows the given numbers of elements apart,
  *             any alignment of the type; draft may be NULL
  *   tokens [n_rows], row_start [n_seqs + 1], out [n_rows], accepted [n_seqs] int32;

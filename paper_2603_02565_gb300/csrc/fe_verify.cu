@@ -5,9 +5,9 @@
 // drawn from: w = p, or max(p - q, 0) (p without y where there is no q) after a rejection, and
 //   the first i with sum_{k <= i} w_k > u sum_k w_k.
 // A whole number comes out, so the sums have to be alike however they are split: each w goes
-// into them as a whole number of units of 2^-45.  Two additions of a constant round w to
-// 2^-22, and what is left over of it (with what p - q in 32 bits leaves over) to 2^-45; 32-bit integer sums of both
-// parts are exact, and need no 64-bit float, of which the GPU has two a clock and SM.
+// into them as a whole number of units of 2^-45.  Adding 1 rounds p - q to 2^-23, and adding a small constant to what is left over
+// of it (within 2^-24 + 2^-25) rounds that to 2^-45; 32-bit integer sums of both parts are exact, and need no 64-bit float, of
+// which the GPU has two a clock and SM.
 //
 // A cluster of CTAs has a sequence, each a run of its row's 16-byte pieces, each warp a run of that.
 // The CTAs add up their sums through shared memory, the warp whose run has the threshold goes
@@ -43,15 +43,16 @@ constexpr int kCtas = sizeof(T) == 4 && !FEW ? 6 : 4;
 constexpr uint32_t kOne = 0x3f800000u;
 
 struct Sum {
-  unsigned long long hi;  // units of 2^-22
+  unsigned long long hi;  // units of 2^-23
   long long lo;           // units of 2^-45
-  __device__ __forceinline__ unsigned long long all() const { return (hi << 23) + (unsigned long long)lo; }
+  __device__ __forceinline__ unsigned long long all() const { return (hi << 22) + (unsigned long long)lo; }
 };
 
-// A w in [0, 1] added to kTop leaves it in steps of 2^-22 in the sum's last bits; what is left over, within half such a step,
-// added to kLow, in steps of 2^-45.
-constexpr float kTop = 2.f, kLow = 0x1.8p-22f;
-constexpr uint32_t kTopBits = 0x40000000u, kLowBits = 0x34c00000u;
+// A w in [0, 1] added to kTop leaves it in steps of 2^-23 in the sum's last bits (2, the end of the range, follows on from those below
+// it).  What is left over, up to half such a step and what 32 bits could not hold of p - q (2^-25 at most), added to kLow, leaves
+// that in steps of 2^-45: the sum stays within 2^-22 .. 2^-21, where such steps are.
+constexpr float kTop = 1.f, kLow = 0x1.8p-22f;
+constexpr uint32_t kTopBits = 0x3f800000u, kLowBits = 0x34c00000u;
 
 // What a token is drawn from: with q max(p - q, 0), otherwise p, and 0 at `but`
 template <typename T, bool FEW>
@@ -67,19 +68,17 @@ struct Weights {
   __device__ __forceinline__ static void weights(float x0, float x1, float y0, float y1, uint32_t& hi, uint32_t& lo, uint32_t& worst) {
     const uint64_t top = f32x2_pack(kTop, kTop), low = f32x2_pack(kLow, kLow), one = f32x2_pack(-1.f, -1.f);
     worst = max(max(worst, __float_as_uint(x0)), __float_as_uint(x1));
-    uint64_t w, e;
-    if (Q) {
-      // max(p - q, 0) as max(p, q) - q, and what 32 bits leave over of it (exact, for max(p, q) >= q >= 0)
+    const uint64_t m = Q ? f32x2_pack(fmaxf(x0, y0), fmaxf(x1, y1)) : f32x2_pack(x0, x1);
+    uint64_t w = m, q = 0;
+    if (Q) {  // max(p - q, 0) as max(p, q) - q
       worst = max(max(worst, __float_as_uint(y0)), __float_as_uint(y1));
-      const uint64_t q = f32x2_pack(y0, y1), m = f32x2_pack(fmaxf(x0, y0), fmaxf(x1, y1));
+      q = f32x2_pack(y0, y1);
       w = f32x2_fma(q, one, m);
-      e = f32x2_fma(q, one, f32x2_fma(w, one, m));
-    } else {
-      w = f32x2_pack(x0, x1);
     }
     const uint64_t a = f32x2_add(w, top);
-    uint64_t left = f32x2_fma(f32x2_fma(top, one, a), one, w);
-    if (Q) left = f32x2_add(left, e);
+    // m less the rounded w is exact: a multiple of m's last bit, and no larger than m or 2^-24.  Less q it is rounded, by 2^-48 at most.
+    uint64_t left = f32x2_fma(f32x2_fma(top, one, a), one, m);
+    if (Q) left = f32x2_fma(q, one, left);
     const uint64_t b = f32x2_add(left, low);
     float a0, a1, b0, b1;
     f32x2_unpack(a, a0, a1);
@@ -311,8 +310,8 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, FEW>) verify_kernel(const V
     cluster_wait();
   }
   const unsigned long long sum = all.all();
-  // (a sum of 2^17 or more would not fit 64 bits)
-  if (worst > kOne || sum == 0 || (all.hi >> (22 + 17)) != 0) {
+  // (units of 2^-45 of a sum below 2^17 fit 64 bits)
+  if (worst > kOne || sum == 0 || (all.hi >> (23 + 17)) != 0) {
     if (first) {
       p.out[t] = -1;
       if (p.status) atomicOr(p.status, FE_ST_INDEX);
