@@ -131,7 +131,11 @@ struct Weights {
     uint32_t h = 0u - N * kTopBits, l = 0u - N * kLowBits;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      x[i] = i < upto && e0 + i != but ? __fadd_rn(x[i], 0.f) : 0.f;  // (no -0)
+      x[i] = i < upto ? __fadd_rn(x[i], 0.f) : 0.f;  // (no -0)
+      if (e0 + i == but) {
+        worst = max(worst, __float_as_uint(x[i]));
+        x[i] = 0.f;
+      }
       y[i] = q && i < upto ? __fadd_rn(y[i], 0.f) : 0.f;
     }
 #pragma unroll
