@@ -366,8 +366,8 @@ __device__ __forceinline__ uint32_t top_scale(uint8_t* tile, float* ks, bool mix
 }
 
 // Query row r of the unit, of a lane 8 elements of each group, as f16 times 2^k, which is returned: the largest comes to
-// 2^14 .. 2^15 (a row without a number above 0: k = 0).  put(b, words): group b in the order of the codes' masks, every second
-// element a sixteenth.
+// 2^14 .. 2^15 (a row without a number above 0: k = 0).  A row that holds an infinity is NaN throughout, or scores of -inf alone
+// would leave no weight.  put(b, words): group b in the order of the codes' masks, every second element a sixteenth.
 template <typename T, int D, typename Put>
 __device__ __forceinline__ int load_query(const NibbleParams& p, const Unit& u, int r, int t, Put put) {
   constexpr int G = D / 32;
@@ -387,7 +387,7 @@ __device__ __forceinline__ int load_query(const NibbleParams& p, const Unit& u, 
   big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
   int k = 0;
   if (big > 0.f && big < INFINITY) k = min(14 - ilogbf(big), 120);
-  const float up = ldexpf(1.f, k);
+  const float up = big == INFINITY ? NAN : ldexpf(1.f, k);
 #pragma unroll
   for (int b = 0; b < G; ++b) {
     float f[8];

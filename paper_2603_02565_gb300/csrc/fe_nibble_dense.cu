@@ -360,10 +360,11 @@ __global__ void __launch_bounds__(kThreads, 2) dense_kernel(const NibbleParams p
             for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(f[i]));
           }
         }
-        // times a power of two that brings the largest to 2^14 .. 2^15 (a row without a number above 0: times 1)
+        // times a power of two that brings the largest to 2^14 .. 2^15 (a row without a number above 0: times 1); a row that holds an
+        // infinity is NaN throughout, or scores of -inf alone would leave no weight
         int k = 0;
         if (big > 0.f && big < INFINITY) k = min(14 - ilogbf(big), 120);
-        const float up = ldexpf(1.f, k);
+        const float up = big == INFINITY ? NAN : ldexpf(1.f, k);
         sc = fmaxf(ldexpf(p.sc, 3 - k), 1e-37f);  // (keys are an eighth)
 #pragma unroll 2
         for (int c = 0; c < D / 8; ++c) {
