@@ -25,9 +25,11 @@
 //   sequences below 226 us, 222 so, and log-sums two to three times as far off.)
 //   Keys: queries are f16 times a power of two, which holds bf16 to 2^-35 of the row's largest; every second element's is
 //   a sixteenth.  The groups' sums are fp32, scales come to them.
-//   Values: scales go to the weights, p s in f16: p is rounded by 2^-11, p s again.  The reference
-//   of the weights follows the largest scale, so that p s ends below 2^15 and counts down to 2^-24.  Their sum is that of
-//   the rounded weights, by a product with ones; the log-sum's that of the exact ones, in fp32.
+//   Values: scales go to the weights, p s in f16: p is rounded by 2^-11, p s again.  Very small and large scales are lifted or
+//   lowered by a power of two, and the reference of the weights follows the largest, so that p s ends below 2^15 and a long flat
+//   tail keeps its weight under a peak.  (A peak over 131071 keys of 2^-17 to 2^-19 of its weight: off by up to 12 % at scales of
+//   2^-14 and 55 % at 65504 when scales stayed as they are; 222 us instead of 226 for the 64 sequences below.)
+//   The weights' sum is that of the rounded ones, by a product with ones; the log-sum's that of the exact ones, in fp32.
 //
 // What bounds it: a half tile's chain of dependent steps in the 12 or 16 warps that registers allow an SM; they issue in 52 to 56 %
 // of the cycles, the tensor pipe is busy for 18 to 24.  GB300, a call alone in a replayed graph, caches flushed:
@@ -171,6 +173,8 @@ struct alignas(16) Unit {
   int head, group, t0, r0, rows, plen, ptiles;  // plen: the prefix's end
   int pfirst, ofirst;                           // first key of the prefix and of the own rows (those before: the dense part's)
   int own_keys, all_see, first_seq, alone;      // own keys of the list; those that all rows see; all rows are of first_seq
+  uint32_t cap;                                 // what the values' scales so far ask for,
+  float base;                                   // and where weights start, in log2
   int seq[32], seen[32], start[32], orow[32];   // its sequence, own keys that it sees, first of its keys in the own list, row of
                                                 // out / head 0
 };
@@ -291,11 +295,32 @@ struct KeyLoader {
   }
 };
 
-// The largest of a tile's scales of values (as f16 has it); key: key `lane` of a mixed tile.  Keys that are none, or that make
-// their rows NaN by their score, get scales of 0.  spoil(key, groups): a key whose scales of these groups are no numbers.
-// The keys' scales go to ks in fp32, infinities as NaN.
-template <int D, typename Spoil>
-__device__ __forceinline__ uint32_t top_scale(uint8_t* tile, float* ks, bool mixed, int2 key, Spoil spoil) {
+// What the scales of values seen so far ask for goes by `cap`, the largest scale (as f16 has it) that asks for no more:
+// scales are lifted by a power of two (2^lift_of) that brings the largest to 2^-8 .. 1, or below 2^8 if it is beyond, and weights
+// start at 2^(25 - exponent_of), so that a weight times a scale is below 2^15 with the slack of new_reference.  Both are at least 2^3
+// for the largest, and f16's smallest step is 2^-24: what is not rounded to 11 bits is held to 2^-28 of the largest.  (Scales
+// of some 2^-8 to 1, values of 0.03 to 7, need neither.)
+constexpr uint32_t kSmallest = 0xffu, kUsual = 0x3bffu;
+__device__ __forceinline__ uint32_t cap_of(uint32_t top) {  // borders 2^-16, 2^-8, 1
+  return top < 0x100u ? kSmallest : top < 0x1c00u ? 0x1bffu : top < 0x3c00u ? kUsual : top | 0x3ffu;
+}
+__device__ __forceinline__ int lift_of(uint32_t cap) {  // and 2^8, 2^12
+  return cap < 0x100u ? 16 : cap < 0x1c00u ? 8 : cap < 0x5c00u ? 0 : cap < 0x6c00u ? -4 : -8;
+}
+__device__ __forceinline__ int exponent_of(uint32_t cap) { return cap < 0x3c00u ? 14 : (int)(cap >> 10) + lift_of(cap); }
+__device__ __forceinline__ float power_of_2(int e) { return __int_as_float((127 + e) << 23); }
+// (by one lane, before the first tile of a unit's piece)
+__device__ __forceinline__ void start_scales(Unit* u) {
+  u->cap = kSmallest;
+  u->base = 25 - exponent_of(kSmallest);
+}
+
+// A tile's scales before it is used: the keys' go to ks in fp32, infinities as NaN, the values' are lifted.  key: key `lane` of a mixed
+// tile.  Keys that are none, or that make their rows NaN by their score, get scales of 0.  gate: up to this the largest scale asks for
+// nothing (-1: all are lifted).  spoil(key, groups): a key whose scales of these groups are no numbers.  renew(lower, units): weights are
+// 2^lower of what they were from here on, and the sums of weighted values count in these units of the old ones.
+template <int D, typename Spoil, typename Renew>
+__device__ __forceinline__ void take_scales(uint8_t* tile, float* ks, bool mixed, int2 key, Unit* u, int& gate, Spoil spoil, Renew renew) {
   using L = Tile<D>;
   constexpr int G = D / 32, W = D == 128 ? 2 : 1;  // W: words of a key's scales
   const int lane = threadIdx.x & 31;
@@ -336,33 +361,48 @@ __device__ __forceinline__ uint32_t top_scale(uint8_t* tile, float* ks, bool mix
     put_scales();
   }
   top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
-  if (top >= 0x7c00u) {
-    // Scales that are negative, or no numbers: these spoil their group in the rows that see the key (a masked weight is
-    // 0, and would too), and count as 0.
-    top = 0;
-    uint32_t wrong = 0;  // groups of key `lane`
+  if ((int)top > gate) {
+    if (top >= 0x7c00u) {
+      // Scales that are negative, or no numbers: these spoil their group in the rows that see the key (a masked weight is
+      // 0, and would too), and count as 0.
+      top = 0;
+      uint32_t wrong = 0;  // groups of key `lane`
 #pragma unroll
-    for (int b = 0; b < G; ++b) {
-      const uint32_t y = (vw[b / 2] >> (16 * (b & 1))) & 0x7fffu;
-      if (y < 0x7c00u) {
-        top = max(top, y);
-      } else {
-        wrong |= 1u << b;
-        vw[b / 2] &= b & 1 ? 0x0000ffffu : 0xffff0000u;
+      for (int b = 0; b < G; ++b) {
+        const uint32_t y = (vw[b / 2] >> (16 * (b & 1))) & 0x7fffu;
+        if (y < 0x7c00u) {
+          top = max(top, y);
+        } else {
+          wrong |= 1u << b;
+          vw[b / 2] &= b & 1 ? 0x0000ffffu : 0xffff0000u;
+        }
+      }
+      top = __reduce_max_sync(0xffffffffu, top);
+#pragma unroll 1
+      for (uint32_t left = __ballot_sync(0xffffffffu, wrong != 0); left; left &= left - 1) {
+        const int i = __ffs(left) - 1;
+        const int2 k = make_int2(__shfl_sync(0xffffffffu, key.x, i), __shfl_sync(0xffffffffu, key.y, i));
+        const uint32_t groups = __shfl_sync(0xffffffffu, wrong, i);
+        spoil(k, groups);
       }
     }
-    put_scales();
-    top = __reduce_max_sync(0xffffffffu, top);
-#pragma unroll 1
-    for (uint32_t left = __ballot_sync(0xffffffffu, wrong != 0); left; left &= left - 1) {
-      const int i = __ffs(left) - 1;
-      const int2 k = make_int2(__shfl_sync(0xffffffffu, key.x, i), __shfl_sync(0xffffffffu, key.y, i));
-      const uint32_t groups = __shfl_sync(0xffffffffu, wrong, i);
-      spoil(k, groups);
+    const uint32_t old = u->cap, cap = max(old, cap_of(top));
+    __syncwarp();
+    const int lift = lift_of(cap);
+    if (cap != old) {
+      renew((float)(exponent_of(old) - exponent_of(cap)), power_of_2(lift - lift_of(old)));
+      if (lane == 0) {
+        u->cap = cap;
+        u->base = 25 - exponent_of(cap);
+      }
     }
+    gate = lift == 0 ? (int)cap : -1;
+    const uint32_t f = (uint32_t)(15 + min(lift, 8)) * 0x04000400u, f2 = lift > 8 ? 0x5c005c00u : 0x3c003c00u;  // (f16 has no 2^16)
+#pragma unroll
+    for (int i = 0; i < W; ++i) vw[i] = mul2(mul2(vw[i], f), f2);
+    put_scales();
   }
   __syncwarp();  // (scales that have been written)
-  return top;
 }
 
 // Query row r of the unit, of a lane 8 elements of each group, as f16 times 2^k, which is returned: the largest comes to
@@ -466,20 +506,23 @@ __device__ __forceinline__ void value_words(const uint8_t* tile, int h, int g, i
     }
   }
 }
-// A weight is 2^(y + nm), y = s qs the score in log2 units, nm = 25 - e - m: m follows the row's maximum by kSlack, e is the
-// exponent of the largest scale of values so far (as f16 has it, 14 at least), so that a weight is below 2^15, and times a scale, too.
-// Scores are compared as they are summed, s: lim = (m + kSlack) / qs.  This takes a new largest score and exponent in, and
-// returns what to multiply the row's sums by.
+// A weight is 2^(y + nm), y = s qs the score in log2 units, nm = 25 - e - m: m follows the row's maximum by kSlack, e is exponent_of
+// the scales so far (14 at least), so that a weight is below 2^15, and times a scale, too.  Scores are compared as they are
+// summed, s: lim = (m + kSlack) / qs.  This takes a new largest score in, and returns what to multiply the row's sums by.
 constexpr float kSlack = 4.f;
-__device__ __forceinline__ float new_reference(float most, float qs, int e, int e1, float& lim, float& nm) {
+__device__ __forceinline__ float new_reference(float most, float qs, float base, float& lim, float& nm) {
   const float old = nm;
   if (most > lim) {
     lim = most + __fdividef(kSlack, qs);
-    nm = (float)(25 - e1) - most * qs;
-  } else if (nm != kNoMax) {
-    nm += (float)(e - e1);
+    nm = base - most * qs;
   }
   return ex2_approx(nm - old);  // (0 where there was no maximum, and nothing)
+}
+// The same for weights that are 2^lower of what they were (nm is rounded: by what it has changed)
+__device__ __forceinline__ float lower_reference(float lower, float& nm) {
+  const float old = nm;
+  if (nm != kNoMax) nm += lower;
+  return ex2_approx(nm - old);
 }
 // The warps' runs: equal ones of all units' tiles, by weight.  A tile is the warp's whose run its beginning lies in; runs are as long as
 // the heaviest tile at least, so that the pieces of a unit are those of warps in a row.
@@ -501,16 +544,16 @@ struct Runs {
 __device__ __forceinline__ SplitRec split_record(const NibbleParams& p, const Unit& u, long long last, int w, long long total) {
   return SplitRec{Runs(p, total).of(last) - w + 1, u.t0, u.r0, u.rows, u.head};
 }
-// The end of row r's piece: statistics are written (by the lane that `write`s); f and fs, what its sums and those of the dense part, if
-// `more`, are to be multiplied by; at, its row of out
+// The end of row r's piece, whose sums count in `unit`s: statistics are written (by the lane that `write`s); f and fs, what its sums and those
+// of the dense part, if `more`, are to be multiplied by; at, its row of out
 struct RowEnd {
   int at;
   float f, fs;
   bool more;
 };
 __device__ __forceinline__ RowEnd row_end(const NibbleParams& p, const Unit& u, int r, int off, bool direct, bool write, float nm, float sum,
-                                          float exact, long long slot) {
-  RowEnd z = {u.orow[r] + u.head * p.hr, 0x1p24f, 0.f, off == 0 && (u.pfirst > 0 || u.ofirst > 0)};
+                                          float exact, float unit, long long slot) {
+  RowEnd z = {u.orow[r] + u.head * p.hr, unit, 0.f, off == 0 && (u.pfirst > 0 || u.ofirst > 0)};
   float ref = sum == 0.f ? -INFINITY : -nm;
   if (z.more) {  // the first piece takes what the dense part has made of its keys
     const float2 ml = p.state_ml[z.at];
@@ -557,7 +600,8 @@ __device__ __forceinline__ void attend8(const NibbleParams& p, Unit* up, int off
     hseen[i] = u.seen[2 * t + i];
   }
   float o[G][2][4], lim[2], nm[2], l[4], lx[2];  // l: the rounded weights' sums, twice; lx: the exact ones'
-  int e = 14;
+  int gate = -1;
+  if (lane == 0) start_scales(up);
 #pragma unroll
   for (int i = 0; i < 2; ++i) lim[i] = -kNoMax, nm[i] = kNoMax, lx[i] = 0.f;
 #pragma unroll
@@ -579,7 +623,7 @@ __device__ __forceinline__ void attend8(const NibbleParams& p, Unit* up, int off
     const bool mixed = flags.x != 0;
     int2 key = {-1, 0};  // key `lane`
     if (mixed) key = *reinterpret_cast<const int2*>(tile + L::kMeta + 8 * lane);
-    const uint32_t top = top_scale<D>(tile, ks, mixed, key, [&](int2 k, uint32_t groups) {
+    auto spoil = [&](int2 k, uint32_t groups) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const bool see = seen(k, i);
@@ -587,7 +631,25 @@ __device__ __forceinline__ void attend8(const NibbleParams& p, Unit* up, int off
         for (int b = 0; b < G; ++b)
           if (see && ((groups >> b) & 1)) o[b][0][i] = o[b][0][i + 2] = o[b][1][i] = o[b][1][i + 2] = NAN;
       }
-    });
+    };
+    auto renew = [&](float lower, float units) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float f = lower_reference(lower, nm[i]);
+        l[i] *= f;
+        l[i + 2] *= f;
+        lx[i] *= f;
+        f *= units;
+#pragma unroll
+        for (int b = 0; b < G; ++b) {
+          o[b][0][i] *= f;
+          o[b][0][i + 2] *= f;
+          o[b][1][i] *= f;
+          o[b][1][i + 2] *= f;
+        }
+      }
+    };
+    take_scales<D>(tile, ks, mixed, key, up, gate, spoil, renew);
     // Half a tile at a time (16 keys): long enough, and short code: pieces are often of a few tiles only.
 #pragma unroll 1
     for (int h = 0; h < flags.y; ++h) {
@@ -622,14 +684,13 @@ __device__ __forceinline__ void attend8(const NibbleParams& p, Unit* up, int off
         }
       }
       // ---- weights ----
-      if (__any_sync(0xffffffffu, (int)(top >> 10) > e || fmaxf(s[0], s[2]) > lim[0] || fmaxf(s[1], s[3]) > lim[1])) {
-        const int e1 = max(e, (int)(top >> 10));
+      if (__any_sync(0xffffffffu, fmaxf(s[0], s[2]) > lim[0] || fmaxf(s[1], s[3]) > lim[1])) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           float y = fmaxf(s[i], s[i + 2]);
 #pragma unroll
           for (int z = 4; z < 32; z <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, z));
-          const float f = new_reference(y, qs[i], e, e1, lim[i], nm[i]);
+          const float f = new_reference(y, qs[i], u.base, lim[i], nm[i]);
           l[i] *= f;
           l[i + 2] *= f;
           lx[i] *= f;
@@ -641,7 +702,6 @@ __device__ __forceinline__ void attend8(const NibbleParams& p, Unit* up, int off
             o[b][1][i + 2] *= f;
           }
         }
-        e = e1;
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[i] = ex2_approx(fmaf(s[i], qs[i & 1], nm[i & 1]));
@@ -678,7 +738,7 @@ __device__ __forceinline__ void attend8(const NibbleParams& p, Unit* up, int off
     for (int z = 4; z < 32; z <<= 1) exact += __shfl_xor_sync(0xffffffffu, exact, z);
     if (u.seen[r] < 0) sum = exact = NAN;
     if (r < u.rows) {
-      const RowEnd z = row_end(p, u, r, off, direct, g == 0, nm[i], sum, exact, slot);
+      const RowEnd z = row_end(p, u, r, off, direct, g == 0, nm[i], sum, exact, power_of_2(24 - lift_of(u.cap)), slot);
 #pragma unroll
       for (int b = 0; b < G; ++b) {
         // elements 4 g .. 4 g + 3 of the group
@@ -727,7 +787,8 @@ __device__ __forceinline__ void attend16(const NibbleParams& p, Unit* up, int of
     qs[i] = fmaxf(ldexpf(p.sc, 24 - k), 1e-37f);
   }
   float o[G][4][4], lim[2], nm[2], l[4], lx[2];
-  int e = 14;
+  int gate = -1;
+  if (lane == 0) start_scales(up);
 #pragma unroll
   for (int i = 0; i < 2; ++i) lim[i] = -kNoMax, nm[i] = kNoMax, lx[i] = 0.f;
 #pragma unroll
@@ -749,7 +810,7 @@ __device__ __forceinline__ void attend16(const NibbleParams& p, Unit* up, int of
     const bool mixed = flags.x != 0;
     int2 key = {-1, 0};  // key `lane`
     if (mixed) key = *reinterpret_cast<const int2*>(tile + L::kMeta + 8 * lane);
-    const uint32_t top = top_scale<D>(tile, ks, mixed, key, [&](int2 k, uint32_t groups) {
+    auto spoil = [&](int2 k, uint32_t groups) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const bool see = seen(k.x, k.y, i);
@@ -760,7 +821,25 @@ __device__ __forceinline__ void attend16(const NibbleParams& p, Unit* up, int of
             for (int c = 0; c < 4; ++c) o[b][c][2 * i] = o[b][c][2 * i + 1] = NAN;
           }
       }
-    });
+    };
+    auto renew = [&](float lower, float units) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float f = lower_reference(lower, nm[i]);
+        l[2 * i] *= f;
+        l[2 * i + 1] *= f;
+        lx[i] *= f;
+        f *= units;
+#pragma unroll
+        for (int b = 0; b < G; ++b)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            o[b][c][2 * i] *= f;
+            o[b][c][2 * i + 1] *= f;
+          }
+      }
+    };
+    take_scales<D>(tile, ks, mixed, key, up, gate, spoil, renew);
 #pragma unroll 1
     for (int h = 0; h < flags.y; ++h) {
       int slot = lane;  // (made anew each time: queries that the compiler keeps in registers over the loop cost others their place)
@@ -802,14 +881,13 @@ __device__ __forceinline__ void attend16(const NibbleParams& p, Unit* up, int of
       float most[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) most[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1]));
-      if (__any_sync(0xffffffffu, (int)(top >> 10) > e || most[0] > lim[0] || most[1] > lim[1])) {
-        const int e1 = max(e, (int)(top >> 10));
+      if (__any_sync(0xffffffffu, most[0] > lim[0] || most[1] > lim[1])) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           float y = most[i];
           y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 1));
           y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 2));
-          const float f = new_reference(y, qs[i], e, e1, lim[i], nm[i]);
+          const float f = new_reference(y, qs[i], u.base, lim[i], nm[i]);
           l[2 * i] *= f;
           l[2 * i + 1] *= f;
           lx[i] *= f;
@@ -821,7 +899,6 @@ __device__ __forceinline__ void attend16(const NibbleParams& p, Unit* up, int of
               o[b][c][2 * i + 1] *= f;
             }
         }
-        e = e1;
       }
 #pragma unroll
       for (int z = 0; z < 2; ++z)
@@ -862,7 +939,7 @@ __device__ __forceinline__ void attend16(const NibbleParams& p, Unit* up, int of
     exact += __shfl_xor_sync(0xffffffffu, exact, 2);
     if (u.seen[r] < 0) sum = exact = NAN;
     if (r < u.rows) {
-      const RowEnd z = row_end(p, u, r, off, direct, t == 0, nm[i], sum, exact, slot);
+      const RowEnd z = row_end(p, u, r, off, direct, t == 0, nm[i], sum, exact, power_of_2(24 - lift_of(u.cap)), slot);
 #pragma unroll
       for (int b = 0; b < G; ++b) {
         // elements 8 t .. 8 t + 7 of the group
