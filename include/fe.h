@@ -581,7 +581,7 @@ int fe_nibble_read(const fe_nibble_read_args* args, void* stream);
  * query rows a group on average (sequences times rows times query heads of a key head), for
  * the keys that all rows of a group see, in whole tiles of 128, values are rounded to 11
  * bits instead of weights times scales (to 2^-22 at least), weights down to 2^-32 of the
- * largest; for bf16, if lse is not asked for, keys as values.
+ * largest; keys are held to 2^-22, or for bf16, if lse is not asked for, as values are.
  * Pieces are joined in a fixed order; where work is split follows from all lengths of a
  * call, so a row's last bits may differ with its neighbours.
  */

@@ -27,8 +27,8 @@
 //   a sixteenth.  The groups' sums are fp32, scales come to them.
 //   Values: scales go to the weights, p s in f16: p is rounded by 2^-11, p s again.  Very small and large scales are lifted or
 //   lowered by a power of two, and the reference of the weights follows the largest, so that p s ends below 2^15 and a long flat
-//   tail keeps its weight under a peak.  (A peak over 131071 keys of 2^-17 to 2^-19 of its weight: off by up to 12 % at scales of
-//   2^-14 and 55 % at 65504 when scales stayed as they are; 222 us instead of 226 for the 64 sequences below.)
+//   tail keeps its weight under a peak.  (A peak over 131071 keys of 2^-17 to 2^-18.5 of its weight: off by 3 % at scales of
+//   2^-14, 55 % at 2^-24 and 12 % at 60000 when scales stayed as they are; 222 us instead of 226 for the 64 sequences below.)
 //   The weights' sum is that of the rounded ones, by a product with ones; the log-sum's that of the exact ones, in fp32.
 //
 // What bounds it: a half tile's chain of dependent steps in the 12 or 16 warps that registers allow an SM; they issue in 52 to 56 %

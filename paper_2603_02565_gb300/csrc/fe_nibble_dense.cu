@@ -8,7 +8,8 @@
 //   O += P V    weights 2^(x - m) in f16 from TMEM, values n s / 8 rounded to f16 (an eighth: the largest scale is 65504)
 // Values are rounded by 2^-11 (where the other kernel rounds weights times scales as much), and so are keys where bf16's results
 // (2^-8) hide it.  f16's would not, nor would the log-sum, which is fp32: with these, what is left over of a key's number (three
-// bits) is a second operand of the same product, and lies in the values' place until then.
+// bits) is a second operand of the same product, and lies in the values' place until then.  Eighths of numbers end at f16's
+// 2^-24, so what is small is held to 2^-22 (half a step, times 8): scales from 2^-11 on lose nothing of a key.
 // Four warps make numbers of codes, a thread a key: its codes come in registers a tile ahead, eight numbers leave as 16
 // bytes.  The order of the elements within eight (0 4 1 5 2 6 3 7) is that of the codes' masks; queries are put in the
 // same order, and outputs back.  Four warps are the softmax, a row a thread; one issues the products.  Two CTAs an SM fill each
