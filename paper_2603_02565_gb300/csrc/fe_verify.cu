@@ -14,9 +14,9 @@
 // through it again (from L2), 32 pieces a step.
 //
 // What bounds it: for few sequences a chain of steps (offsets, tokens, their probabilities; the sums; the cluster; the search),
-// for many the instructions of the sums as well: 7 an element, two at a time.  More loads at once help few rows alone.  GB300, a
-// call alone in a replayed graph, caches flushed: one row of 100003 bf16 16.5 us; 200 sequences of up to 5 drafts over 131072
-// fp32, with draft probabilities, 58.5 us (bytes at a copy's rate: 31); 500 of up to 7 over 32768 f16, without, 27.8 us (4.8).
+// for many the instructions of the sums as well: 7 an element, two at a time.  GB300, a call alone in a replayed graph, caches
+// flushed, here and below: one row of 100003 bf16 14.5 us; 200 sequences of up to 5 drafts over 131072 fp32, with draft
+// probabilities, 54.5 us (bytes at a copy's rate: 31); 500 of up to 7 over 32768 f16, without, 25.5 us (4.8).
 #include <algorithm>
 
 #include "fe_kernels.h"
@@ -35,11 +35,9 @@ struct VerifyParams {
 };
 
 constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCluster = 8;
-// CTAs an SM: registers for a piece of fp32 twice, or of 16 bits, which is eight numbers.  FEW: no more CTAs than fit with
-// four an SM; these have registers for twice the loads at once.  (A row of 131072 fp32: 19.5 us, 21.6 without; 200 rows in
-// eight CTAs each, which do not fit: 62.6 with four an SM, 58.5 with six.)
-template <typename T, bool FEW>
-constexpr int kCtas = sizeof(T) == 4 && !FEW ? 6 : 4;
+// CTAs an SM: registers for several loads at once.  (Six, with half the loads of fp32: a row of 131072 24 us instead of 18, 200 of them
+// 60.5 instead of 55; 500 of 32768 f16 34 instead of 26, and with four loads instead of two 30.)
+constexpr int kCtas = 4;
 constexpr uint32_t kOne = 0x3f800000u;
 
 struct Sum {
@@ -55,7 +53,7 @@ constexpr float kTop = 1.f, kLow = 0x1.8p-22f;
 constexpr uint32_t kTopBits = 0x3f800000u, kLowBits = 0x34c00000u;
 
 // What a token is drawn from: with q max(p - q, 0), otherwise p, and 0 at `but`
-template <typename T, bool FEW>
+template <typename T>
 struct Weights {
   static constexpr int N = 16 / (int)sizeof(T);
   const T *p, *q;
@@ -89,7 +87,7 @@ struct Weights {
   // Pieces ka + lane, ka + lane + 32, ... below kb, all of them whole; `but` is not looked for
   template <bool Q>
   __device__ __forceinline__ void add_whole(int ka, int kb, Sum& v, uint32_t& worst) const {
-    constexpr int U = (FEW && sizeof(T) == 4 ? 2 : 1) * (Q || sizeof(T) == 2 ? 2 : 4);  // loads of each at once
+    constexpr int U = sizeof(T) == 2 ? 2 : Q ? 4 : 8;  // loads of each at once (a piece of 16 bits is eight numbers)
     const uint4* from = reinterpret_cast<const uint4*>(p - mis);
     const uint4* less = reinterpret_cast<const uint4*>(q - (Q ? mis : 0));
     for (int k = ka + (int)(threadIdx.x & 31); k < kb; k += 32 * U) {
@@ -170,8 +168,8 @@ __device__ __forceinline__ unsigned long long remote_u64(const void* p, uint32_t
   return v;
 }
 
-template <typename T, bool FEW>
-__global__ void __launch_bounds__(kThreads, kCtas<T, FEW>) verify_kernel(const VerifyParams p, const int cluster) {
+template <typename T>
+__global__ void __launch_bounds__(kThreads, kCtas) verify_kernel(const VerifyParams p, const int cluster) {
   __shared__ unsigned long long sh_hi[kWarps];
   __shared__ long long sh_lo[kWarps];
   __shared__ uint32_t sh_worst[kWarps];
@@ -228,7 +226,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, FEW>) verify_kernel(const V
     }
     return;
   }
-  Weights<T, FEW> w;
+  Weights<T> w;
   w.p = target + (long long)t * p.target_row;
   w.q = rejected && draft ? draft + (long long)t * p.draft_row : nullptr;
   w.vocab = p.vocab;
@@ -241,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, FEW>) verify_kernel(const V
   auto one = [&](int k, Sum& v) {
     uint32_t hi = 0;
     int32_t lo = 0;
-    w.add(k, Weights<T, FEW>::N, hi, lo, worst);
+    w.add(k, Weights<T>::N, hi, lo, worst);
     v.hi += hi;
     v.lo += lo;
   };
@@ -255,12 +253,12 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, FEW>) verify_kernel(const V
     int ka = k0, kb = k0;
     if (w.whole && !careful) {
       ka = max(k0, w.mis > 0 ? 1 : 0);
-      kb = max(ka, min(k1, (w.vocab + w.mis) / Weights<T, FEW>::N));
+      kb = max(ka, min(k1, (w.vocab + w.mis) / Weights<T>::N));
       if (ka > k0 && k1 > k0 && lane == 0) one(k0, v);
       if (w.q) {
         w.template add_whole<true>(ka, kb, v, worst);
       } else {
-        const int out = w.but < 0 ? kb : min(kb, max(ka, (w.but + w.mis) / Weights<T, FEW>::N));
+        const int out = w.but < 0 ? kb : min(kb, max(ka, (w.but + w.mis) / Weights<T>::N));
         w.template add_whole<false>(ka, out, v, worst);
         if (out < kb && lane == 0) one(out, v);
         w.template add_whole<false>(out + 1, kb, v, worst);
@@ -327,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, FEW>) verify_kernel(const V
       for (int k = k0; k < k1; k += 32) {
         uint32_t hi = 0, unused = 0;
         int32_t lo = 0;
-        if (k + lane < k1) w.add(k + lane, Weights<T, FEW>::N, hi, lo, unused);
+        if (k + lane < k1) w.add(k + lane, Weights<T>::N, hi, lo, unused);
         unsigned long long c = Sum{hi, lo}.all();
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -341,9 +339,9 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, FEW>) verify_kernel(const V
           if (l > 0) before += up;
           // an element a lane: the sum of the piece up to it
           hi = 0, lo = 0;
-          if (lane < Weights<T, FEW>::N) w.add(k + l, lane + 1, hi, lo, unused);
-          const uint32_t at = __ballot_sync(0xffffffffu, lane < Weights<T, FEW>::N && before + Sum{hi, lo}.all() > bound);
-          if (lane == 0) p.out[t] = (k + l) * Weights<T, FEW>::N - w.mis + __ffs(at) - 1;
+          if (lane < Weights<T>::N) w.add(k + l, lane + 1, hi, lo, unused);
+          const uint32_t at = __ballot_sync(0xffffffffu, lane < Weights<T>::N && before + Sum{hi, lo}.all() > bound);
+          if (lane == 0) p.out[t] = (k + l) * Weights<T>::N - w.mis + __ffs(at) - 1;
           break;
         }
         before += __shfl_sync(0xffffffffu, c, 31);
@@ -357,20 +355,18 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, FEW>) verify_kernel(const V
 template <typename T>
 cudaError_t verify_go(const VerifyParams& p, cudaStream_t s) {
   // CTAs a sequence: as many as the SMs hold at once, as long as each thread has a piece of 16 bytes; and until it has no more than
-  // 16 (200 sequences x 131072 fp32: 52 us with eight CTAs each, 59 with four, 70 with two; 500 x 32768 f16: 24 with
-  // one, 31 with two)
+  // 16.  (200 sequences x 131072 fp32: 55 us with eight CTAs each, 60 with four, 81 with two; 500 x 32768 f16, which is 16 pieces: 26
+  // with one, 30 with two, 40 with four; 500 x 50257 f16: 38 with two, 36 with one.  So the step past 16 costs some 4 of 28 us.)
   int cluster = 1, sms = 0;
   const cudaError_t e = device_sms(&sms);
   if (e != cudaSuccess) return e;
   const long long pieces = (long long)p.vocab * (int)sizeof(T) / 16;
   while (cluster < kMaxCluster &&
          (pieces > 16LL * kThreads * cluster ||
-          (pieces > (long long)kThreads * cluster && 2LL * p.n_seqs * cluster <= (long long)kCtas<T, false> * sms)))
+          (pieces > (long long)kThreads * cluster && 2LL * p.n_seqs * cluster <= (long long)kCtas * sms)))
     cluster *= 2;
   const dim3 grid((unsigned)p.n_seqs * cluster);
-  if (sizeof(T) == 4 && (long long)p.n_seqs * cluster <= (long long)kCtas<T, true> * sms)
-    return launch_kc(verify_kernel<T, sizeof(T) == 4>, grid, dim3(kThreads), 0, s, cluster, p, cluster);
-  return launch_kc(verify_kernel<T, false>, grid, dim3(kThreads), 0, s, cluster, p, cluster);
+  return launch_kc(verify_kernel<T>, grid, dim3(kThreads), 0, s, cluster, p, cluster);
 }
 
 }  // namespace
