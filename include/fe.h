@@ -574,6 +574,7 @@ int fe_nibble_read(const fe_nibble_read_args* args, void* stream);
  * all be NULL (n_groups 0): then no prefix is shared, each sequence sees its own rows alone.
  * At most 2^26 rows fit a page table (page_cols * page_rows), and 2^27 sequences or
  * groups a call: FE_ERR_UNSUPPORTED beyond.  Queries that are not finite make their rows NaN.
+ * Scores are to stay below 2^23 in magnitude (fp32 holds nothing of a weight in larger ones).
  * Roundings: scores are fp32 sums of the products of queries and numbers, exact but for
  * queries below 2^-35 of their row's largest; weights are rounded to 11 bits, and again
  * times values' scales, for the product with the values' numbers (each to 2^-28 of the
