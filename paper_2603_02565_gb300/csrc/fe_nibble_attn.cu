@@ -22,7 +22,7 @@
 // little of them; 9 to 16 are the long one.
 //   A code in the low bits of a 16-bit float is u 2^-24, one in the next four 16 u 2^-24: a mask makes two numbers of a word.
 //   8 is taken off in f16 (exactly).  (Of keys, sums that start at -8 sum q saved that, and took registers and digits: the 64
-//   sequences below 226 us, 222 so, and log-sums two to three times as far off.)
+//   sequences below 4 us longer, and log-sums two to three times as far off.)
 //   Keys: queries are f16 times a power of two, which holds bf16 to 2^-35 of the row's largest; every second element's is
 //   a sixteenth.  The groups' sums are fp32, scales come to them.
 //   Values: scales go to the weights, p s in f16: p is rounded by 2^-11, p s again.  Very small and large scales are lifted or
@@ -33,12 +33,13 @@
 //
 // What bounds it: a half tile's chain of dependent steps in the 12 or 16 warps that registers allow an SM; they issue in 52 to 56 %
 // of the cycles, the tensor pipe is busy for 18 to 24.  GB300, a call alone in a replayed graph, caches flushed:
-//   one sequence of 131071 rows, 32 over 8 heads of 128, f16: 59.5 us (bytes at a copy's rate: 22; 16 us of it are what a call
-//   of a few rows takes, and beyond that keys come at 4.5 TB/s; two or three tiles in flight a warp make no difference)
-//   64 sequences of up to 16384 rows, 1 to 5 query rows each, 32 over 8 of 128, bf16: 222 us (bytes 92)
-//   256 x 50 sequences of up to 6 rows, prefixes of 256, 4 of 32, bf16: 84 us with the dense part, 108 without
+//   one sequence of 131071 rows, 32 over 8 heads of 128, f16: 60 us (bytes at a copy's rate: 22; 16 us of it are what a call
+//   of a few rows takes, and beyond that keys come at 4.5 TB/s; a ring of three tiles a warp instead of two: 61)
+//   64 sequences of up to 16384 rows, 1 to 5 query rows each, 32 over 8 of 128, bf16: 226 us (bytes 92)
+//   256 x 50 sequences of up to 6 rows, prefixes of 256, 4 of 32, bf16: 85 us with the dense part, 97 without
 //   the finish kernel is 6 to 10 us of each: 2 to start, 2 for offsets and records, the rest two or three reads that wait on another
-// Steps on the way, for the 64 sequences: 16 keys a tile 428, 32 265, rows as the long side 245, runs by weight 226, numbers of keys instead of codes 222.
+// Steps on the way, for the 64 sequences: 16 keys a tile 428, 32 265, rows as the long side 245, runs by weight 226, numbers of keys instead of
+// codes 222, scales lifted 226.
 #include <cmath>
 
 #include "fe_nibble_attn.cuh"
@@ -48,8 +49,8 @@ namespace {
 
 constexpr int kKeys = 32, kWarps = 4, kThreads = 32 * kWarps;
 
-// What a key tile costs a warp, in parts, by how many rows the unit has.  (64 sequences of up to 5 x 4 rows: 226 us; 230 by
-// 2 : 3, 240 by 3 : 5, 253 without weights.)
+// What a key tile costs a warp, in parts, by how many rows the unit has.  (64 sequences of up to 5 x 4 rows: 226 us; 228 by
+// 2 : 3, 237 by 3 : 5, 249 without weights.)
 __host__ __device__ __forceinline__ constexpr int tile_weight(int rows) { return rows <= 8 ? 3 : 4; }
 
 // Key tiles of a row tile (one head) times their weight: at least 1, or 0 if it is unused.  Lengths that are none count as 0, and are reported.
@@ -1264,8 +1265,17 @@ int check_attention(const fe_nibble_attention_args* a) {
 struct Layout {
   size_t bad, cum, slot_group, recs, part_o, part_ml, stat, dcum, dslot_group, drecs, dpart_o, dpart_ml, state_o, state_ml, bytes;
 };
-// What a call is run with: rows of a unit and warps
+// Rows a group, on average, above which keys that they share go through the dense part.  What a call takes with it, and without |
+// with it and the keys' rest (us, a replayed graph; bf16, 6 own rows a sequence), by rows a group:
+//                                               16             32              48              64
+//   4 prefixes of 32768, 32 over 8 of 128    110, 91 | 141   110, 130 | 147  116, 175 | 147  118, 220 | 149
+//   4 of 8192                                 67, 56 | 74     69, 65 | 77     71, 79 | 78     73, 91 | 81
+//   64 of 1024, 16 over 4 of 64               59, 56 | 65     65, 54 | 69     73, 64 | 75     69, 77 | 73
+//   256 of 256, 4 of 32                       67, 71 | 71     77, 69 | 79     88, 80 | 91     97, 91 | 101
+// So 32 lies between the crossings of long prefixes (20 and 37 rows of the first, 37 and 48 of the second) and short ones (some 55
+// of the third); a rule that looked at lengths would need them on the host.
 constexpr int kDenseFrom = 32;
+// What a call is run with: rows of a unit and warps
 struct Shape {
   int nt, ctas, groups, slots;
   bool dense;
