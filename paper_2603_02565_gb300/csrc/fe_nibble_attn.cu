@@ -31,8 +31,8 @@
 //   2^-14, 55 % at 2^-24 and 12 % at 60000 when scales stayed as they are; 222 us instead of 226 for the 64 sequences below.)
 //   The weights' sum is that of the rounded ones, by a product with ones; the log-sum's that of the exact ones, in fp32.
 //
-// What bounds it: a half tile's chain of dependent steps in the 12 or 16 warps that registers allow an SM; they issue in 52 to 56 %
-// of the cycles, the tensor pipe is busy for 18 to 24.  GB300, a call alone in a replayed graph, caches flushed:
+// What bounds it: a half tile's chain of dependent steps in the 12 or 16 warps that registers allow an SM; they issue in 55 to 58 %
+// of the cycles, the tensor pipe is busy for 18 to 25.  GB300, a call alone in a replayed graph, caches flushed:
 //   one sequence of 131071 rows, 32 over 8 heads of 128, f16: 60 us (bytes at a copy's rate: 22; 16 us of it are what a call
 //   of a few rows takes, and beyond that keys come at 4.5 TB/s; a ring of three tiles a warp instead of two: 61)
 //   64 sequences of up to 16384 rows, 1 to 5 query rows each, 32 over 8 of 128, bf16: 226 us (bytes 92)
