@@ -576,13 +576,15 @@ int fe_nibble_read(const fe_nibble_read_args* args, void* stream);
  * groups a call: FE_ERR_UNSUPPORTED beyond.  Queries that are not finite make their rows NaN.
  * Scores are to stay below 2^23 in magnitude (fp32 holds nothing of a weight in larger ones).
  * Roundings: scores are fp32 sums of the products of queries and numbers, exact but for
- * queries below 2^-35 of their row's largest; weights are rounded to 11 bits, and again
- * times values' scales, for the product with the values' numbers (each to 2^-28 of the
- * row's largest at least; so are scales beside one of 2^8 or more).  With more than 32
- * query rows a group on average (sequences times rows times query heads of a key head), for
- * the keys that all rows of a group see, in whole tiles of 128, values are rounded to 11
- * bits instead of weights times scales (to 2^-22 at least), weights down to 2^-32 of the
- * largest; keys are held to 2^-22, or for bf16, if lse is not asked for, as values are.
+ * queries below 2^-35 of their row's largest; weights are rounded to 11 bits, or 2^-28 of the
+ * row's largest, and again times values' scales, for the product with the values' numbers: to
+ * 11 bits, or 2^-28 of the row's largest weight times the largest scale of a value that it or
+ * one of 16 rows of its group and key head sees (scales beside one of 2^8 or more: of that
+ * one).  With more than 32 query rows a group on average (sequences times rows times query
+ * heads of a key head), for the keys that all rows of a group see, in whole tiles of 128,
+ * values are rounded to 11 bits instead of weights times scales (to 2^-22 at least), weights
+ * down to 2^-32 of the largest; keys are held to 2^-22, or for bf16, if lse is not asked for,
+ * as values are.
  * Pieces are joined in a fixed order; where work is split follows from all lengths of a
  * call, so a row's last bits may differ with its neighbours.
  */

@@ -298,9 +298,9 @@ struct KeyLoader {
 
 // What the scales of values seen so far ask for goes by `cap`, the largest scale (as f16 has it) that asks for no more:
 // scales are lifted by a power of two (2^lift_of) that brings the largest to 2^-8 .. 1, or below 2^8 if it is beyond, and weights
-// start at 2^(25 - exponent_of), so that a weight times a scale is below 2^15 with the slack of new_reference.  Both are at least 2^3
-// for the largest, and f16's smallest step is 2^-24: what is not rounded to 11 bits is held to 2^-28 of the largest.  (Scales
-// of some 2^-8 to 1, values of 0.03 to 7, need neither.)
+// start at 2^(25 - exponent_of), so that a weight times a scale is below 2^15 with the slack of new_reference.  A row's largest weight is at
+// least 2^3, so is that times the largest lifted scale, and f16's smallest step is 2^-24: what is not rounded to 11 bits is held to
+// 2^-28 of these.  All rows and groups of a unit go by one scale.  (From 2^-8 to 1, values of 0.03 to 7, nothing is to do.)
 constexpr uint32_t kSmallest = 0xffu, kUsual = 0x3bffu;
 __device__ __forceinline__ uint32_t cap_of(uint32_t top) {  // borders 2^-16, 2^-8, 1
   return top < 0x100u ? kSmallest : top < 0x1c00u ? 0x1bffu : top < 0x3c00u ? kUsual : top | 0x3ffu;
